@@ -1,7 +1,8 @@
 /*
  * qarl.h -- C ABI of the MI355X (gfx950) hot path of QaRL: the low-bit quantized MoE
  * expert GEMM at decode and at prefill / training-forward shapes, the weight quantizer
- * that feeds both, the softmax top-k router, and the per-token log-prob comparison.
+ * that feeds both, the softmax top-k router, and the per-token log-prob comparison; and the rest of
+ * a decoder layer around it: RMS norm, the paged KV cache and attention over it.
  *
  * Conventions (all entry points)
  *   - plain C, no exceptions cross the boundary; the return value is a qarl_status;
@@ -287,6 +288,98 @@ int qarl_tbpo_objective(const float *lp_current, const float *lp_old, const floa
                         float eps_high, float delta_low, float delta_high, float tis_cap_c,
                         float *r_seq, float *w_seq_clipped, float *r_clipped, int32_t *in_band,
                         float *objective_seq, float *objective, float *grad_lp_current, void *stream);
+
+/* ---- The other half of a decoder layer: residual addition with RMS norm, the paged KV cache, attention over it.
+ * Section 3.1's two engines run it around the quantized experts; the paper gives no kernel for it.  Positions are the
+ * caller's: q and k arrive with whatever rotation the model applies. */
+
+/* h = x + residual in fp32 (x alone where residual is NULL), then per row of K
+ *   y = h * rstd * weight,  rstd = 1 / sqrt(mean_k h^2 + eps),
+ * from the fp32 sum, before it is rounded.  Outputs, each of which may be NULL but not all of y, codes and residual_out:
+ *   residual_out [rows][K]  h rounded to the stream's type (the residual of the next addition)
+ *   y_bf16       [rows][K]  y rounded once
+ *   codes uint8 [rows][K] and scales float [rows]: the FP quantizer of section 2.2 applied to the row of y, scale = absmax / 448,
+ *       code = e4m3_rne(y / scale) with IEEE divides: what qarl_qgemm_grouped takes as x and x_scales.  via_bf16 == 0 quantizes
+ *       the fp32 values; via_bf16 != 0 quantizes the values rounded to bf16: the bytes that qarl_quantize_rows_fp8 makes of y_bf16
+ *       and that qarl_qgemm_routed makes of it inside, so that both engines run on the same codes.  A zero row gets scale 0 and
+ *       codes 0; a row with a NaN or an infinity among its y gets scale NaN and NaN codes.
+ * stream_dtype (QARL_OUT_BF16 or QARL_OUT_F32) is the type of residual and residual_out.  Strides are the elements between rows.
+ * residual_out may be residual or x itself, y_bf16 may be x (same pointer and stride); outputs may not overlap inputs otherwise.
+ * Supported: K % 8 == 0, K <= 16384, strides multiples of 8, buffers 16-byte (codes: 8-byte) aligned, eps >= 0 and finite.
+ * rows == 0 is a no-op. */
+int qarl_add_rmsnorm(const void *x_bf16, int64_t x_stride, const void *residual, int64_t residual_stride,
+                     const void *weight_bf16, int64_t rows, int K, float eps, int stream_dtype, void *residual_out,
+                     int64_t residual_out_stride, void *y_bf16, int64_t y_stride, void *codes, float *scales,
+                     int via_bf16, void *stream);
+
+/* Its backward.  h [rows][K] is the sum as stored (residual_out; x for a norm without residual), dy bf16 the gradient of y, dh (may be
+ * NULL) the gradient that reaches h along the residual stream:
+ *   dx = dh + rstd * (dy * weight - h * rstd^2 * mean_k(dy * weight * h)),   the gradient of x and of residual alike,
+ *   dw[k] = sum over the rows of dy * h * rstd    (fp32 sums in a fixed order; dw may be NULL).
+ * Through a quantized output the gradient is the straight-through one: that of y.  h, dh and dx are of stream_dtype, dw of
+ * dw_dtype.  dx may be dh or h itself (same pointer and stride).  ws: qarl_add_rmsnorm_backward_workspace_bytes(rows, K) bytes,
+ * 16-byte aligned, needed for dw only.  Limits as above.  rows == 0: dw is all zeros. */
+size_t qarl_add_rmsnorm_backward_workspace_bytes(int64_t rows, int K);
+int qarl_add_rmsnorm_backward(const void *dy_bf16, int64_t dy_stride, const void *h, int64_t h_stride, const void *dh,
+                              int64_t dh_stride, const void *weight_bf16, int64_t rows, int K, float eps,
+                              int stream_dtype, void *dx, int64_t dx_stride, void *dw, int dw_dtype, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* A paged KV cache.  Host struct, device buffers.  Token position p of a sequence lies in page block_table[p / page_size] at offset
+ * p % page_size; a slot is page * page_size + offset.
+ *   KV_BF16: k, v bf16  [num_pages][kv_heads][page_size][head_dim]
+ *   KV_E4M3: k, v uint8 of the same shape (e4m3 bit patterns), k_scales, v_scales float [num_pages][kv_heads][page_size]: the FP
+ *            quantizer of section 2.2 with one scale per token and head; value = scale * code.
+ * Requirements: head_dim 64 or 128, page_size a power of two from 8 to 1024, kv_heads <= 1024, buffers 16-byte aligned. */
+typedef enum { QARL_KV_BF16 = 1, QARL_KV_E4M3 = 2 } qarl_kv_format;
+typedef struct {
+    int32_t fmt; /* qarl_kv_format */
+    int32_t num_pages, page_size, kv_heads, head_dim;
+    void *k, *v;
+    float *k_scales, *v_scales; /* KV_E4M3 only */
+} qarl_kv_cache;
+
+/* Bytes of k (and of v), of k_scales (and of v_scales); 0 for an unknown format or non-positive sizes. */
+size_t qarl_kv_cache_bytes(int fmt, int num_pages, int page_size, int kv_heads, int head_dim);
+size_t qarl_kv_scales_bytes(int fmt, int num_pages, int page_size, int kv_heads, int head_dim);
+
+/* Writes T tokens into the cache: token t, head h comes from k_bf16 + t * k_token_stride + h * k_head_stride (elements; head_dim
+ * contiguous; v likewise) and goes to slot slots[t]; KV_E4M3 quantizes it on the way (scale = absmax / 448, code = e4m3_rne(x / scale),
+ * IEEE divides; zero rows: scale 0, codes 0; rows with a NaN or an infinity: scale NaN, NaN codes).  A slot outside
+ * [0, num_pages * page_size) is skipped.  Of two tokens with the same slot one or a mixture is kept.
+ * Strides multiples of 8, k and v 16-byte aligned.  T == 0 is a no-op. */
+int qarl_kv_cache_write(const qarl_kv_cache *cache, const void *k_bf16, int64_t k_token_stride, int64_t k_head_stride,
+                        const void *v_bf16, int64_t v_token_stride, int64_t v_head_stride, int64_t T,
+                        const int64_t *slots, void *stream);
+
+/* Reads sequences back in bf16: rows [offsets[s], offsets[s+1]) of k_out and v_out [total][kv_heads][head_dim] are positions 0, 1, ... of
+ * sequence s, whose pages are block_table + s * table_stride, table_width of them.  offsets ascend; rows of no sequence, positions
+ * past the table and pages outside [0, num_pages) read as zeros.  total == 0 is a no-op. */
+int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, int64_t table_stride, int table_width,
+                       const int32_t *offsets, int S, int64_t total, void *k_out_bf16, void *v_out_bf16, void *stream);
+
+/* Causal attention of new tokens over the cache, which holds their keys and values already.  Sequence s has the query rows
+ * [q_offsets[s], q_offsets[s+1]) (n of them: one when it is decoded, a chunk or all of a prompt when it is filled in) and kv_lens[s]
+ * cached positions, the new ones last: query i stands at position p = kv_lens[s] - n + i and sees the positions j with
+ * 0 <= j <= p and, where window > 0, j > p - window.  Query head h reads cached head h / (q_heads / kv_heads):
+ *   out[t][h][:] = sum_j softmax_j(scale * q . k_j) v_j,   lse[t][h] = ln sum_j exp(scale * q . k_j)   (lse may be NULL)
+ * with fp32 scores, maxima and sums; the probabilities (KV_E4M3: times the scale of v_j) are rounded to bf16 once where they meet v.
+ * A query that sees nothing (p < 0: an idle slot of a batch) gets zeros and lse -inf.
+ *   q_bf16 [T][q_heads] rows at q_token_stride and q_head_stride (elements, multiples of 8), 16-byte aligned; out [T][q_heads][head_dim],
+ *   bf16 or fp32 (out_dtype).  Cached values at positions that a query does not see never reach its result, whatever their bits.
+ *   max_q_len, max_kv_len: host bounds of n and of kv_lens[s]; cached positions from max_kv_len on, and from
+ *   table_width * page_size on, are cut off; rows past max_q_len of a sequence may be left unwritten.  Pages outside
+ *   [0, num_pages) hold nothing: their positions are not seen.
+ *   ws: qarl_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (0 for calls that are not split along the cache).
+ * A sequence's cache is split where there are few rows; a row's result depends on its sequence and on (T, S, max_q_len, max_kv_len),
+ * not on timing.  Supported: q_heads % kv_heads == 0, q_heads <= 1024.  T == 0 or S == 0 is a no-op. */
+size_t qarl_paged_attention_workspace_bytes(const qarl_kv_cache *cache, int T, int q_heads, int S, int max_q_len,
+                                            int max_kv_len);
+int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_head_stride, int T, int q_heads,
+                         const qarl_kv_cache *cache, const int32_t *block_table, int64_t table_stride, int table_width,
+                         const int32_t *kv_lens, const int32_t *q_offsets, int S, int max_q_len, int max_kv_len,
+                         float scale, int window, void *out, int out_dtype, float *lse, void *ws, size_t ws_bytes,
+                         void *stream);
 
 #ifdef __cplusplus
 }

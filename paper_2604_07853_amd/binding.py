@@ -22,13 +22,16 @@ E4M3_ACT_FORMATS = (QARL_FP8_E4M3_CH, QARL_FP4_E2M1_CH, QARL_W4A8_G128)   # e4m3
 QARL_PATH_AUTO, QARL_PATH_DECODE, QARL_PATH_PREFILL = 0, 1, 2
 QARL_EPI_NONE, QARL_EPI_SILU_MUL, QARL_EPI_COMBINE = 0, 1, 2
 QARL_OUT_BF16, QARL_OUT_F32 = 0, 1
+QARL_KV_BF16, QARL_KV_E4M3 = 1, 2
 
-# the first six return a string or a size, the rest a qarl_status
-EXPORTS = ["qarl_last_error", "qarl_qgemm_workspace_bytes", "qarl_logprob_workspace_bytes",
+# the first ten return a string or a size, the rest a qarl_status
+EXPORTS = ["qarl_last_error", "qarl_add_rmsnorm_backward_workspace_bytes", "qarl_kv_cache_bytes", "qarl_kv_scales_bytes",
+           "qarl_paged_attention_workspace_bytes", "qarl_qgemm_workspace_bytes", "qarl_logprob_workspace_bytes",
            "qarl_token_logprob_static_limit", "qarl_codes_bytes", "qarl_scales_bytes", "qarl_quantize_weights", "qarl_quantize_rows_fp8", "qarl_moe_route", "qarl_qgemm_grouped",
            "qarl_qgemm_routed", "qarl_moe_layer_routed", "qarl_token_logprob", "qarl_logprob_mismatch", "qarl_tbpo_objective",
            "qarl_token_logprob_static", "qarl_codes_to_canonical", "qarl_qgemm_grouped_dx",
-           "qarl_grouped_dw"]
+           "qarl_grouped_dw", "qarl_add_rmsnorm", "qarl_add_rmsnorm_backward", "qarl_kv_cache_write", "qarl_kv_cache_read",
+           "qarl_paged_attention"]
 
 
 class QarlError(RuntimeError):
@@ -40,6 +43,12 @@ class QarlError(RuntimeError):
 class qarl_qweight(C.Structure):
     _fields_ = [("fmt", C.c_int32), ("E", C.c_int32), ("N", C.c_int32), ("K", C.c_int32),
                 ("group", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class qarl_kv_cache(C.Structure):
+    _fields_ = [("fmt", C.c_int32), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p),
+                ("v_scales", C.c_void_p)]
 
 
 _lib = None
@@ -88,7 +97,20 @@ def lib():
                                                 C.c_void_p, C.c_void_p, C.c_void_p]
         L.qarl_token_logprob_static_limit.restype = C.c_size_t
         L.qarl_token_logprob_static_limit.argtypes = []
-        for name in EXPORTS[6:]:
+        i64, vp, i32, f32, sz = C.c_int64, C.c_void_p, C.c_int, C.c_float, C.c_size_t
+        L.qarl_add_rmsnorm.argtypes = [vp, i64, vp, i64, vp, i64, i32, f32, i32, vp, i64, vp, i64, vp, vp, i32, vp]
+        L.qarl_add_rmsnorm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.qarl_add_rmsnorm_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, f32, i32, vp, i64, vp, i32, vp, sz, vp]
+        for fn in (L.qarl_kv_cache_bytes, L.qarl_kv_scales_bytes):
+            fn.argtypes = [i32] * 5
+        L.qarl_kv_cache_write.argtypes = [C.POINTER(qarl_kv_cache), vp, i64, i64, vp, i64, i64, i64, vp, vp]
+        L.qarl_kv_cache_read.argtypes = [C.POINTER(qarl_kv_cache), vp, i64, i32, vp, i32, i64, vp, vp, vp]
+        L.qarl_paged_attention_workspace_bytes.argtypes = [C.POINTER(qarl_kv_cache)] + [i32] * 5
+        L.qarl_paged_attention.argtypes = [vp, i64, i64, i32, i32, C.POINTER(qarl_kv_cache), vp, i64, i32, vp, vp, i32, i32, i32, f32,
+                                           i32, vp, i32, vp, vp, sz, vp]
+        for name in EXPORTS[1:5]:
+            getattr(L, name).restype = C.c_size_t
+        for name in EXPORTS[10:]:
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -407,3 +429,188 @@ def qarl_tbpo_objective(lp_current, lp_old, lp_sampler, seq_offsets, advantage, 
     if want_grad:
         out["grad"] = g
     return out
+
+
+def _dtype_code(t):
+    return QARL_OUT_F32 if t.dtype == torch.float32 else QARL_OUT_BF16
+
+
+def _rows(t, name, dtypes, shape):
+    """(pointer, stride) of a matrix whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype not in dtypes or t.shape != shape or (shape[0] and shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be %s on the GPU, of type %s, with contiguous rows (got %s, %s)"
+                         % (name, list(shape), " or ".join(map(str, dtypes)), list(t.shape), t.dtype))
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+
+
+def _flat(t, name, dtype, shape):
+    """Pointer of a contiguous tensor; None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be %s on the GPU, contiguous, of type %s (got %s, %s)" % (name, list(shape), dtype, list(t.shape), t.dtype))
+    return t.data_ptr()
+
+
+_BF16, _STREAM = (torch.bfloat16,), (torch.bfloat16, torch.float32)
+
+
+def qarl_add_rmsnorm(x, weight, eps, residual=None, residual_out=None, y=None, codes=None, scales=None, quantize=False, via_bf16=False):
+    """y = rmsnorm(x + residual) * weight in bf16 and / or as e4m3 codes and row scales; see include/qarl.h.  x [rows, K] bf16, residual
+    and residual_out [rows, K] bf16 or fp32.  Allocates residual_out where there is a residual, codes and scales with
+    quantize=True, y where neither is asked for.  Returns dict(y, codes, scales, residual)."""
+    rows, K = x.shape
+    dev = x.device
+    if residual is not None and residual_out is None:
+        residual_out = torch.empty((rows, K), dtype=residual.dtype, device=dev)
+    if quantize and codes is None:
+        codes = torch.empty((rows, K), dtype=torch.uint8, device=dev)
+    if codes is not None and scales is None:
+        scales = torch.empty((rows,), dtype=torch.float32, device=dev)
+    if y is None and codes is None:
+        y = torch.empty((rows, K), dtype=torch.bfloat16, device=dev)
+    if residual is not None and residual_out.dtype != residual.dtype:
+        raise ValueError("residual and residual_out have different types")
+    shape = (rows, K)
+    xp, xs = _rows(x, "x", _BF16, shape)
+    rp, rs = _rows(residual, "residual", _STREAM, shape)
+    op, os_ = _rows(residual_out, "residual_out", _STREAM, shape)
+    yp, ys = _rows(y, "y", _BF16, shape)
+    st = residual_out if residual_out is not None else residual
+    _check(lib().qarl_add_rmsnorm(xp, xs, rp, rs, _flat(weight, "weight", torch.bfloat16, (K,)), rows, K, eps,
+                                  QARL_OUT_BF16 if st is None else _dtype_code(st), op, os_, yp, ys,
+                                  _flat(codes, "codes", torch.uint8, shape), _flat(scales, "scales", torch.float32, (rows,)),
+                                  int(via_bf16), torch.cuda.current_stream().cuda_stream))
+    return dict(y=y, codes=codes, scales=scales, residual=residual_out)
+
+
+def qarl_add_rmsnorm_backward_workspace_bytes(rows, K):
+    return lib().qarl_add_rmsnorm_backward_workspace_bytes(rows, K)
+
+
+def qarl_add_rmsnorm_backward(dy, h, weight, eps, dh=None, dx=None, dw=None, want_dw=True, dw_dtype=QARL_OUT_F32, ws=None):
+    """Gradients of qarl_add_rmsnorm: dx (of x and of residual) in h's type and dw; see include/qarl.h.  dh: the gradient arriving along
+    the residual stream.  Allocates dx, dw (want_dw) and ws when not given.  Returns dict(dx, dw)."""
+    rows, K = h.shape
+    dev = h.device
+    shape = (rows, K)
+    if dx is None:
+        dx = torch.empty(shape, dtype=h.dtype, device=dev)
+    if dw is None and want_dw:
+        dw = torch.empty((K,), dtype=torch.float32 if dw_dtype == QARL_OUT_F32 else torch.bfloat16, device=dev)
+    if dw is not None and ws is None:
+        ws = torch.empty((lib().qarl_add_rmsnorm_backward_workspace_bytes(rows, K),), dtype=torch.uint8, device=dev)
+    same = (h.dtype,)
+    yp, ys = _rows(dy, "dy", _BF16, shape)
+    hp, hs = _rows(h, "h", _STREAM, shape)
+    gp, gs = _rows(dh, "dh", same, shape)
+    xp, xs = _rows(dx, "dx", same, shape)
+    if dw is not None and dw.dtype not in _STREAM:
+        raise ValueError("dw must be bf16 or fp32 (got %s)" % dw.dtype)
+    _check(lib().qarl_add_rmsnorm_backward(yp, ys, hp, hs, gp, gs, _flat(weight, "weight", torch.bfloat16, (K,)), rows, K, eps,
+                                           _dtype_code(h), xp, xs, None if dw is None else _flat(dw, "dw", dw.dtype, (K,)),
+                                           QARL_OUT_F32 if dw is None else _dtype_code(dw), None if ws is None else ws.data_ptr(),
+                                           0 if ws is None else ws.numel() * ws.element_size(), torch.cuda.current_stream().cuda_stream))
+    return dict(dx=dx, dw=dw)
+
+
+class KVCache:
+    """A paged KV cache: the tensors plus the C descriptor.  k, v [num_pages, kv_heads, page_size, head_dim], bf16 or (with k_scales and
+    v_scales, fp32 [num_pages, kv_heads, page_size]) uint8 e4m3 codes."""
+
+    def __init__(self, fmt, k, v, k_scales=None, v_scales=None):
+        if fmt not in (QARL_KV_BF16, QARL_KV_E4M3):
+            raise ValueError("unknown cache format %r" % (fmt,))
+        dt = torch.uint8 if fmt == QARL_KV_E4M3 else torch.bfloat16
+        for t in (k, v):
+            if t.dtype != dt or t.dim() != 4 or t.shape != k.shape or not t.is_contiguous():
+                raise ValueError("k and v must be contiguous %s tensors of one shape [pages, heads, page size, head dim]" % dt)
+        if fmt == QARL_KV_E4M3:
+            for t in (k_scales, v_scales):
+                if t is None or t.dtype != torch.float32 or t.shape != k.shape[:3] or not t.is_contiguous():
+                    raise ValueError("k_scales and v_scales must be contiguous fp32 tensors %s" % list(k.shape[:3]))
+        self.fmt, self.k, self.v, self.k_scales, self.v_scales = fmt, k, v, k_scales, v_scales
+        self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.desc = qarl_kv_cache(fmt, self.num_pages, self.page_size, self.kv_heads, self.head_dim, k.data_ptr(), v.data_ptr(),
+                                  k_scales.data_ptr() if fmt == QARL_KV_E4M3 else None, v_scales.data_ptr() if fmt == QARL_KV_E4M3 else None)
+
+    @staticmethod
+    def empty(fmt, num_pages, page_size, kv_heads, head_dim, device="cuda"):
+        shape = (num_pages, kv_heads, page_size, head_dim)
+        if fmt == QARL_KV_E4M3:
+            codes = [torch.empty(shape, dtype=torch.uint8, device=device) for _ in range(2)]
+            scales = [torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2)]
+            return KVCache(fmt, *codes, *scales)
+        return KVCache(fmt, *[torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)])
+
+
+def _heads(t, name, shape):
+    """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose heads are contiguous."""
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.shape != shape or t.stride(2) != 1:
+        raise ValueError("%s must be bf16 %s on the GPU with contiguous heads (got %s, %s)" % (name, list(shape), list(t.shape), t.dtype))
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _table(t, S):
+    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != S or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("block_table must be int32 [%d, pages] on the GPU with contiguous rows (got %s, %s)" % (S, list(t.shape), t.dtype))
+    return t.data_ptr(), t.stride(0) if S > 1 else t.shape[1], t.shape[1]
+
+
+def qarl_kv_cache_write(cache, k, v, slots):
+    """Writes k, v [T, kv_heads, head_dim] (bf16, any token and head stride) into the slots [T] (int64) of the cache; see include/qarl.h."""
+    shape = (slots.numel(), cache.kv_heads, cache.head_dim)
+    kp, kt, kh = _heads(k, "k", shape)
+    vp, vt, vh = _heads(v, "v", shape)
+    _check(lib().qarl_kv_cache_write(C.byref(cache.desc), kp, kt, kh, vp, vt, vh, shape[0],
+                                     _flat(slots, "slots", torch.int64, (shape[0],)), torch.cuda.current_stream().cuda_stream))
+
+
+def qarl_kv_cache_read(cache, block_table, offsets, total, out=None):
+    """(k, v) bf16 [total, kv_heads, head_dim]: positions 0, 1, ... of every sequence, sequence s in rows [offsets[s], offsets[s+1]);
+    see include/qarl.h.  `total` is the host's copy of offsets[-1]."""
+    shape = (total, cache.kv_heads, cache.head_dim)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=block_table.device) for _ in range(2))
+    k, v = out
+    S = offsets.numel() - 1
+    tp, ts, tw = _table(block_table, S)
+    _check(lib().qarl_kv_cache_read(C.byref(cache.desc), tp, ts, tw, _flat(offsets, "offsets", torch.int32, (S + 1,)), S, total,
+                                    _flat(k, "k", torch.bfloat16, shape), _flat(v, "v", torch.bfloat16, shape),
+                                    torch.cuda.current_stream().cuda_stream))
+    return k, v
+
+
+def qarl_paged_attention_workspace_bytes(cache, T, q_heads, S, max_q_len, max_kv_len):
+    return lib().qarl_paged_attention_workspace_bytes(C.byref(cache.desc), T, q_heads, S, max_q_len, max_kv_len)
+
+
+def qarl_paged_attention(query, cache, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, scale=None, window=0, out=None,
+                         out_dtype=QARL_OUT_BF16, lse=None, want_lse=False, ws=None):
+    """Causal attention of query [T, q_heads, head_dim] (bf16, any token and head stride) over the cache; see include/qarl.h.  scale is
+    head_dim ** -0.5 unless given.  Allocates out, lse (want_lse) and ws when not given.  Returns dict(out, lse)."""
+    T, Hq, D = query.shape
+    dev = query.device
+    shape = (T, Hq, cache.head_dim)
+    S = kv_lens.numel()
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32 if out_dtype == QARL_OUT_F32 else torch.bfloat16, device=dev)
+    elif out.dtype not in _STREAM:
+        raise ValueError("out must be bf16 or fp32 (got %s)" % out.dtype)
+    if lse is None and want_lse:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+    qp, qt, qh = _heads(query, "query", shape)
+    tp, ts, tw = _table(block_table, S)
+    L, desc = lib(), C.byref(cache.desc)
+    if ws is None:
+        need = L.qarl_paged_attention_workspace_bytes(desc, T, Hq, S, max_q_len, max_kv_len)
+        if need:
+            ws = torch.empty((need,), dtype=torch.uint8, device=dev)
+    _check(L.qarl_paged_attention(qp, qt, qh, T, Hq, desc, tp, ts, tw, _flat(kv_lens, "kv_lens", torch.int32, (S,)),
+                                  _flat(q_offsets, "q_offsets", torch.int32, (S + 1,)), S, max_q_len, max_kv_len,
+                                  D ** -0.5 if scale is None else scale, window, _flat(out, "out", out.dtype, shape), _dtype_code(out),
+                                  _flat(lse, "lse", torch.float32, (T, Hq)), None if ws is None else ws.data_ptr(),
+                                  0 if ws is None else ws.numel() * ws.element_size(), torch.cuda.current_stream().cuda_stream))
+    return dict(out=out, lse=lse)

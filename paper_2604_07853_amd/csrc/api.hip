@@ -40,8 +40,6 @@ int raise_lds_limit(const void *kernel, LdsLimitOnce &done, const char *what)
     return QARL_OK;
 }
 
-static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-
 static int check_qweight(const qarl_qweight *w, const char *who)
 {
     if (!w) {

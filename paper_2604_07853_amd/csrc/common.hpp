@@ -150,6 +150,68 @@ __device__ __forceinline__ u32x2 e4m3_quantize_bf16x8(const RowScale &rs, u32x4 
     return o;
 }
 
+// The same quantizer for rows whose scale differs between the lanes of a wavefront, and for fp32 values.  absmax8 folds eight
+// values into a running absmax that is +inf once a value is an infinity or a NaN (fmaxf alone would drop the NaN); quantize8
+// then gives NaN codes, and the scale to store is lane_scale().
+struct LaneScale {
+    float s, y;
+    bool fast, bad;
+    __device__ __forceinline__ explicit LaneScale(float absmax) : s(absmax / 448.0f), y(1.0f / s)
+    {
+        bad = !(absmax < __builtin_inff());
+        fast = s >= 0x1p-100f && s < 0x1p100f && (__float_as_uint(s) & 0x7fffffu) != 0x7fffffu;
+    }
+    __device__ __forceinline__ static float absmax8(const float (&t)[8], float am)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) am = fabsf(t[i]) <= am ? am : (t[i] == t[i] ? fabsf(t[i]) : __builtin_inff());
+        return am;
+    }
+    __device__ __forceinline__ float stored() const { return bad ? __builtin_nanf("") : s; }
+    __device__ __forceinline__ u32x2 quantize8(const float (&x)[8]) const
+    {
+        if (bad) return u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+        if (s == 0.f) return u32x2{0, 0};
+        float t[8];
+        if (fast) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q0 = x[i] * y;
+                t[i] = copysignf(fmaf(fmaf(-q0, s, x[i]), y, q0), x[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = x[i] / s;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = __builtin_amdgcn_fmed3f(t[i], -448.f, 448.f);
+        u32x2 o;
+        int w0 = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+        o[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], w0, true);
+        int w1 = __builtin_amdgcn_cvt_pk_fp8_f32(t[4], t[5], 0, false);
+        o[1] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[6], t[7], w1, true);
+        return o;
+    }
+};
+
+__device__ __forceinline__ void bf16x8_to_f32(u32x4 v, float (&t)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        t[2 * i] = __uint_as_float(v[i] << 16);
+        t[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+}
+
+// Eight fp32 values -> bf16, round to nearest even
+__device__ __forceinline__ u32x4 f32_to_bf16x8(const float (&t)[8])
+{
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (uint32_t)f32_to_bf16_hw(t[2 * i]) | (uint32_t)f32_to_bf16_hw(t[2 * i + 1]) << 16;
+    return o;
+}
+
 // Eight e4m3 bytes -> the bf16 values they stand for (exact: four significant bits).
 __device__ __forceinline__ u32x4 e4m3_as_bf16x8(u32x2 q8)
 {
@@ -302,6 +364,8 @@ inline bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb)
     return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
+inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
 // Host-side error plumbing (api.hip).
 void set_error(const char *fmt, ...);
 int check_hip(hipError_t e, const char *what);
@@ -394,6 +458,66 @@ int launch_tbpo(const float *lp_cur, const float *lp_old, const float *lp_smp, c
                 const float *adv, float eps_low, float eps_high, float delta_low, float delta_high, float c,
                 float *r_seq, float *w_clip, float *r_clip, int32_t *in_band, float *obj_seq, float *objective,
                 float *grad, hipStream_t s);
+// The attention half of a layer (rmsnorm.hip, kv_cache.hip, attention.hip); validated in api_attention.hip
+struct NormArgs {
+    const void *x;           // bf16
+    const void *res;         // stream type, or null
+    const void *w;           // bf16
+    int64_t x_stride, res_stride, res_out_stride, y_stride;
+    int64_t rows;
+    int K;
+    float eps;
+    int stream_f32;
+    void *res_out;           // stream type, or null
+    void *y;                 // bf16, or null
+    void *codes;             // e4m3 [rows][K], or null
+    float *scales;
+    int via_bf16;
+};
+int launch_rmsnorm(const NormArgs &a, hipStream_t s);
+struct NormGradArgs {
+    const void *dy, *h, *dh, *w;     // dh may be null
+    int64_t dy_stride, h_stride, dh_stride, dx_stride;
+    int64_t rows;
+    int K;
+    float eps;
+    int stream_f32;
+    void *dx;
+    void *dw;                        // or null
+    int dw_f32;
+    float *partials;                 // [rmsnorm_backward_groups(rows, K)][K]
+};
+int64_t rmsnorm_backward_groups(int64_t rows, int K);
+int launch_rmsnorm_backward(const NormGradArgs &a, hipStream_t s);
+struct KvArgs {
+    int fmt;
+    int num_pages, page_shift, kv_heads, head_dim;   // page_size = 1 << page_shift
+    void *k, *v;
+    float *k_scales, *v_scales;
+};
+int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, const void *v, int64_t vts, int64_t vhs, int64_t T,
+                    const int64_t *slots, hipStream_t s);
+int launch_kv_read(const KvArgs &c, const int32_t *table, int64_t table_stride, int table_width, const int32_t *offsets, int S,
+                   int64_t total, void *k_out, void *v_out, hipStream_t s);
+struct AttnArgs {
+    KvArgs kv;
+    const void *q;
+    int64_t q_token_stride, q_head_stride;
+    int T, q_heads;
+    const int32_t *table;
+    int64_t table_stride;
+    int table_width;
+    const int32_t *kv_lens, *q_offsets;
+    int S, max_q_len, max_kv_len;
+    float scale;
+    int window;
+    void *out;
+    int out_f32;
+    float *lse;              // or null
+    void *ws;
+};
+size_t attention_ws_bytes(int T, int q_heads, int kv_heads, int head_dim, int S, int max_q_len, int max_kv_len);
+int launch_attention(const AttnArgs &a, hipStream_t s);
 int launch_mismatch(const float *lp_a, const float *lp_b, int T, const int32_t *seq_offsets, int S, float c,
                     float *delta, float *token_w, float *seq_w, float *seq_wc, hipStream_t s);
 
