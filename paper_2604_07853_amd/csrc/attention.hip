@@ -1,114 +1,106 @@
-// Causal attention of new tokens over the paged cache.  For query row (t, h) at position p, with z_j = scale q.k_j over the visible j:
-//   m = max z, l = sum e^(z_j - m), out = sum e^(z_j - m) v_j / l, lse = m + ln l;
-// the maximum and the sum run along (a block of tokens rescales what the blocks before have left), so the scores are never stored.
-#include "common.hpp"
+// Attention over the paged cache: how a call is split between the kernels and along the cache, and the join of the pieces.
+#include "attention.hpp"
 
 namespace qarl {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
-
-// A wavefront per (token, query head), 64 cached tokens at a time, one per lane for the scores; for the values a lane owns
-// D / 64 of the outputs.
-template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void attention_rows_kernel(AttnArgs a)
+// Sequences with at most 64 rows per cached head go to the kernel whose wavefronts share a sequence's positions, others to the one whose wavefronts
+// share its rows.  Both cut a cache into pieces where there are not enough (sequence, head, row block)s to fill the 256 CUs; partial results cost
+// 2 D fp32 per row and piece, so pieces are not shorter than that is worth.
+static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_q_len, int max_kv_len, int window)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t = (int)(unit / a.q_heads), h = (int)(unit - (int64_t)t * a.q_heads);
-    if (t >= a.T) return;
-    if (t < a.q_offsets[0] || t >= a.q_offsets[a.S]) return;
-    int lo = 0, hi = a.S;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.q_offsets[mid] <= t) lo = mid;
-        else hi = mid;
+    AttnPlan p = {};
+    const int64_t G = q_heads / kv_heads;
+    const int64_t most = min((int64_t)max_q_len, (int64_t)T);
+    const bool all_few = most * G <= 64;
+    const int64_t few_rows = all_few ? most * G : G;         // beside long chunks: single tokens
+    p.few_nr = few_rows <= 16 ? 1 : few_rows <= 32 ? 2 : few_rows <= 64 ? 4 : 0;
+    // can a sequence be that short, where the others are at most `most` long?
+    if (!all_few && T > (int64_t)(S - 1) * most + 16 * p.few_nr / G) p.few_nr = 0;
+    p.tile = !all_few;
+    int64_t len = max_kv_len > 0 ? max_kv_len : 1;
+    const auto cut = [](int64_t length, int64_t items, int64_t wanted, int64_t least, int64_t unit, int64_t most_len, int &chunk, int &splits) {
+        int64_t n = (wanted + items - 1) / items;
+        n = min(n, (length + least - 1) / least);
+        n = n < 1 ? 1 : n;
+        int64_t c = ((length + n - 1) / n + unit - 1) / unit * unit;
+        c = min(max(c, least), most_len);
+        chunk = (int)c;
+        splits = (int)((length + c - 1) / c);
+    };
+    if (window > 0) len = min(len, (int64_t)window + most + kManyTile);
+    if (p.few_nr) cut(len, (int64_t)S * kv_heads, 2048, 256, 128, 8192, p.few_chunk, p.few_splits);
+    if (p.tile) {
+        p.tile_blocks = (int)((T * G + kManyRows - 1) / kManyRows + min((int64_t)S, (int64_t)T));
+        cut(len, (int64_t)p.tile_blocks * kv_heads, 512, 512, 64, (int64_t)1 << 30, p.tile_chunk, p.tile_splits);
     }
-    const int n = a.q_offsets[lo + 1] - a.q_offsets[lo];
-    const int64_t cap = min((int64_t)a.max_kv_len, (int64_t)a.table_width << a.kv.page_shift);
-    const int p = a.kv_lens[lo] - n + (t - a.q_offsets[lo]);
-    const int end = (int)min((int64_t)p + 1, cap);
-    const int begin = a.window > 0 ? max(0, p - a.window + 1) : 0;
-    const int kvh = h / (a.q_heads / a.kv.kv_heads);
-    const uint16_t *q = (const uint16_t *)a.q + (int64_t)t * a.q_token_stride + (int64_t)h * a.q_head_stride;
-    float acc[D / 64] = {};
-    float m = -__builtin_inff(), l = 0.f;
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        const int j = j0 + lane;
-        int64_t row = -1;
-        float z = -__builtin_inff();
-        if (j < end) {
-            const int page = a.table[lo * a.table_stride + (j >> a.kv.page_shift)];
-            if (page >= 0 && page < a.kv.num_pages)
-                row = (((int64_t)page * a.kv.kv_heads + kvh) << a.kv.page_shift) + (j & ((1 << a.kv.page_shift) - 1));
-        }
-        float vs = 1.f;
-        if (row >= 0) {
-            float dot = 0.f;
-            for (int d = 0; d < D; d += 8) {
-                float qf[8], kf[8];
-                bf16x8_to_f32(*(const u32x4 *)(q + d), qf);
-                if (E4M3) bf16x8_to_f32(e4m3_as_bf16x8(*(const u32x2 *)((const uint8_t *)a.kv.k + row * D + d)), kf);
-                else bf16x8_to_f32(*(const u32x4 *)((const uint16_t *)a.kv.k + row * D + d), kf);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dot = fmaf(qf[e], kf[e], dot);
-            }
-            if (E4M3) {
-                dot *= a.kv.k_scales[row];
-                vs = a.kv.v_scales[row];
-            }
-            z = dot * (a.scale * kLog2e);
-        }
-        float mn = z;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor(mn, o, 64));
-        mn = fmaxf(mn, m);
-        const float base = mn == -__builtin_inff() ? 0.f : mn;
-        const float keep = exp2f(m - base);
-        const float pr = row >= 0 ? exp2f(z - base) : 0.f;
-        l = l * keep + wave_sum(pr);
-        m = mn;
-#pragma unroll
-        for (int u = 0; u < D / 64; ++u) acc[u] *= keep;
-        const unsigned long long some = __ballot(row >= 0);
-        for (int k = 0; k < 64; ++k) {
-            if (!(some >> k & 1ull)) continue;
-            const int64_t rk = __shfl(row, k, 64);
-            const float pk = __shfl(pr, k, 64) * __shfl(vs, k, 64);
-#pragma unroll
-            for (int u = 0; u < D / 64; ++u) {
-                const int d = lane + 64 * u;
-                float v;
-                if (E4M3) v = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)a.kv.v)[rk * D + d], 0);
-                else v = bf16_bits_to_f32(((const uint16_t *)a.kv.v)[rk * D + d]);
-                acc[u] = fmaf(pk, v, acc[u]);
-            }
-        }
-    }
-    const float inv = l > 0.f ? 1.0f / l : (l == l ? 0.f : l);
-    const int64_t o = ((int64_t)t * a.q_heads + h) * D;
-#pragma unroll
-    for (int u = 0; u < D / 64; ++u) {
-        if (a.out_f32) ((float *)a.out)[o + lane + 64 * u] = acc[u] * inv;
-        else ((uint16_t *)a.out)[o + lane + 64 * u] = f32_to_bf16_hw(acc[u] * inv);
-    }
-    if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + h] = (m + log2f(l)) * kLn2;
+    p.splits = p.few_splits > p.tile_splits ? p.few_splits : p.tile_splits;
+    if (p.splits <= 1) p.splits = 0;
+    return p;
 }
 
-size_t attention_ws_bytes(int T, int q_heads, int kv_heads, int head_dim, int S, int max_q_len, int max_kv_len) { return 0; }
+static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+size_t attention_ws_bytes(int T, int q_heads, int kv_heads, int head_dim, int S, int max_q_len, int max_kv_len)
+{
+    // a window makes the caches shorter, never the number of pieces larger: a piece more for the rounding
+    const AttnPlan p = attention_plan(T, q_heads, kv_heads, S, max_q_len, max_kv_len, 0);
+    if (!p.splits) return 0;
+    const size_t rows = (size_t)T * q_heads, n = (size_t)p.splits + 1;
+    return up256(n * rows * head_dim * 4) + up256(n * rows * 8) + up256(rows * 4);
+}
+
+// out = sum over the pieces of 2^(m_i - m) O_i / sum of 2^(m_i - m) l_i, in the order of the pieces.  D / 4 lanes per row.
+template <int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, AttnParts parts)
+{
+    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / (D / 4);
+    const int d = (int)(threadIdx.x % (D / 4)) * 4;
+    if (row >= parts.rows) return;
+    const int t = (int)(row / a.q_heads);
+    if (t < a.q_offsets[0] || t >= a.q_offsets[a.S]) return;     // a row of no sequence
+    const int n = min(parts.count[row], parts.splits);
+    if (n <= 1) return;                                          // written where it was computed
+    float top = kNegInf;
+    for (int i = 0; i < n; ++i) top = fmaxf(top, parts.ml[((int64_t)i * parts.rows + row) * 2]);
+    const float tb = top == kNegInf ? 0.f : top;
+    float sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const int64_t at = (int64_t)i * parts.rows + row;
+        const float f = __builtin_amdgcn_exp2f(parts.ml[at * 2] - tb);
+        sum += f * parts.ml[at * 2 + 1];
+        o += *(const f32x4 *)(parts.o + at * D + d) * f;
+    }
+    store_out4(a, row, D, d, o * inverse_sum(sum));
+    if (d == 0 && a.lse) a.lse[row] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
 
 int launch_attention(const AttnArgs &a, hipStream_t s)
 {
-    const int64_t units = (int64_t)a.T * a.q_heads;
-    const dim3 grid((unsigned)((units + 3) / 4)), block(256);
-    const bool e4m3 = a.kv.fmt == QARL_KV_E4M3;
-    if (a.kv.head_dim == 128) {
-        if (e4m3) attention_rows_kernel<128, true><<<grid, block, 0, s>>>(a);
-        else attention_rows_kernel<128, false><<<grid, block, 0, s>>>(a);
-    } else {
-        if (e4m3) attention_rows_kernel<64, true><<<grid, block, 0, s>>>(a);
-        else attention_rows_kernel<64, false><<<grid, block, 0, s>>>(a);
+    const int D = a.kv.head_dim;
+    AttnPlan p = attention_plan(a.T, a.q_heads, a.kv.kv_heads, a.S, a.max_q_len, a.max_kv_len, a.window);
+    AttnParts parts = {};
+    parts.rows = (int64_t)a.T * a.q_heads;
+    if (p.splits) {
+        const size_t n = (size_t)p.splits;
+        parts.splits = p.splits;
+        parts.o = (float *)a.ws;
+        parts.ml = (float *)((char *)a.ws + up256(n * parts.rows * D * 4));
+        parts.count = (int32_t *)((char *)parts.ml + up256(n * parts.rows * 8));
     }
-    return check_hip(hipGetLastError(), "attention_rows_kernel");
+    int rc = QARL_OK;
+    if (p.tile && (rc = launch_attention_tile(a, p, parts, s))) return rc;
+    if (p.few_nr && (rc = launch_attention_few(a, p, parts, s))) return rc;
+    if (!p.splits) return QARL_OK;
+    const int64_t blocks = (parts.rows * (D / 4) + 255) / 256;
+    if (blocks > 0x7fffffffLL) {
+        set_error("qarl_paged_attention: %lld rows exceed the grid limit", (long long)parts.rows);
+        return QARL_ERR_UNSUPPORTED;
+    }
+    if (D == 128) attention_join_kernel<128><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, parts);
+    else attention_join_kernel<64><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, parts);
+    return check_hip(hipGetLastError(), "attention_join_kernel");
 }
 
 }  // namespace qarl
