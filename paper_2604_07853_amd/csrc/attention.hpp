@@ -13,7 +13,7 @@
 namespace qarl {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((address_space(3))) const char *LdsPtr;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr float kNegInf = -__builtin_inff();
@@ -31,7 +31,7 @@ struct AttnPlan {
 
 constexpr int kFewTile = 32;      // positions a wavefront of the few-row kernel takes at a time
 constexpr int kManyTile = 64;     // positions of a tile of the many-row kernel
-constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves;
+constexpr int kManyWaves = 8, kManyRows = 256;
 
 // Partial results in the workspace: O [splits][T * q_heads][D], then (m, l) [splits][T * q_heads], then the number of pieces [T * q_heads]
 struct AttnParts {
@@ -78,34 +78,28 @@ __device__ __forceinline__ void row_bounds(const AttnArgs &a, const SeqRange &s,
     lo = a.window > 0 ? (int)max((int64_t)0, p - a.window + 1) : 0;
 }
 
-// Bits that are set somewhere where a bf16 of the words gathered in `seen` (by gather_nonfinite) is an infinity or a NaN
-__device__ __forceinline__ uint32_t gather_nonfinite(uint32_t seen, uint32_t w) { return seen | ((w & 0x7f807f80u) + 0x00800080u); }
-__device__ __forceinline__ bool any_nonfinite(uint32_t seen) { return (seen & 0x80008000u) != 0; }
-
-// The values of a fragment where they are finite, and bf16 ones where they are not: up for +inf and NaN, down for -inf and NaN.  A matrix
-// product with the rows' 0 / 1 visibility counts them, so that a value that a row does not see cannot reach it (0 * inf is NaN).
-__device__ __forceinline__ void split_nonfinite(bf16x8 v, bf16x8 &fine, bf16x8 &up, bf16x8 &down)
+// A word of bf16 pairs (of four e4m3 codes) with zeros for infinities and NaN (NaN)
+__device__ __forceinline__ uint32_t only_finite_bf16(uint32_t w)
 {
-    const u32x4 w = __builtin_bit_cast(u32x4, v);
-    u32x4 f, u, d;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[i] = u[i] = d[i] = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t e = (w[i] >> (16 * h)) & 0xffffu;
-            const bool bad = (e & 0x7f80u) == 0x7f80u, nan = bad && (e & 0x7fu) != 0;
-            f[i] |= (bad ? 0u : e) << (16 * h);
-            u[i] |= (bad && (nan || e < 0x8000u) ? 0x3f80u : 0u) << (16 * h);
-            d[i] |= (bad && (nan || e >= 0x8000u) ? 0x3f80u : 0u) << (16 * h);
-        }
-    }
-    fine = __builtin_bit_cast(bf16x8, f);
-    up = __builtin_bit_cast(bf16x8, u);
-    down = __builtin_bit_cast(bf16x8, d);
+    const uint32_t bad = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;     // the top bit of a half: its exponent is all ones
+    return w & ~((bad - (bad >> 15)) | bad);
+}
+__device__ __forceinline__ uint32_t only_finite_e4m3(uint32_t w)
+{
+    const uint32_t bad = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;     // the top bit of a byte: its code is 0x7f or 0xff
+    return w & ~((bad - (bad >> 7)) | bad);
 }
 
-__device__ __forceinline__ bf16x8 pack_bf16x8(const float (&p)[8]) { return __builtin_bit_cast(bf16x8, f32_to_bf16x8(p)); }
+// Eight fp32 -> bf16, nearest even (two per instruction)
+__device__ __forceinline__ bf16x8 pack_bf16x8(const float (&p)[8])
+{
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
+    return __builtin_bit_cast(bf16x8, o);
+}
 
 // Eight e4m3 codes -> bf16 (exact; checked for all 256 codes on gfx950)
 __device__ __forceinline__ bf16x8 widen_e4m3x8(uint32_t lo, uint32_t hi)

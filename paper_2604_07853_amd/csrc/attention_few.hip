@@ -122,6 +122,7 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
     row_bounds(a, sr, 0, unused, all_hi);
     row_bounds(a, sr, sr.n - 1, all_lo, unused);
 
+    bool rare = false;      // values that are not finite were found in a tile that some row does not see whole
     const int mine = tiles > wave ? (tiles - wave + kFewWaves - 1) / kFewWaves : 0;
 #pragma unroll
     for (int i = 0; i < L::kRing - 1; ++i)
@@ -222,100 +223,103 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             }
             l[n] += sum;
         }
-        // ---- values
-        auto frag = [&](int dt) -> bf16x8 {
+        // ---- values.  Where rows see different positions (or a page is missing), a value that one of them does not see may be an infinity or a NaN,
+        // and its product with the probability 0 a NaN: such values become zeros in LDS, and the rows that see them get them in the end.  Single tokens
+        // see the same positions in all their rows, and what lies outside those was read from one of them.
+        if (masked && (holes || sr.n > 1)) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < L::kHalf / 1024; ++i) {
+                u32x4 *w = (u32x4 *)(ring + slot * L::kStage + L::kHalf) + i * 64 + lane;
+                u32x4 v = *w;
+                const u32x4 was = v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = E4M3 ? only_finite_e4m3(v[e]) : only_finite_bf16(v[e]);
+                if (v[0] != was[0] || v[1] != was[1] || v[2] != was[2] || v[3] != was[3]) {
+                    *w = v;
+                    bad = true;
+                }
+            }
+            if (E4M3) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(fabsf(vs[e >> 2][e & 3]) < __builtin_inff())) {
+                        vs[e >> 2][e & 3] = 0.f;
+                        bad = true;
+                    }
+            }
+            rare |= __ballot(bad) != 0;
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            if (E4M3) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pv[n][e] *= vs[e >> 2][e & 3];
+            }
+            pf[n] = pack_bf16x8(pv[n]);
+        }
+        // (the reads and their wait in one block: the compiler would let a transposing read that it can see wait for the copies in flight)
+#pragma unroll
+        for (int d4 = 0; d4 < DT; d4 += 4) {
+            bf16x8 v[4];
             if (E4M3) {
                 const int r = ((m16 >> 1) & 3) + 4 * q + 16 * (m16 >> 3);
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                    (__attribute__((address_space(3))) i32x2 *)(st + L::kHalf + r * L::kRowBytes + ((dt ^ L::swz(r)) * 16) + (m16 & 1) * 8));
-                return widen_e4m3x8((uint32_t)w[0], (uint32_t)w[1]);
-            }
-            union {
-                s16x4 half[2];
-                bf16x8 v;
-            } f;
+                const uint32_t at = (uint32_t)(uintptr_t)(LdsPtr)st + L::kHalf + r * L::kRowBytes + (L::swz(r) * 16) + (m16 & 1) * 8;
+                u32x2 w[4];
+                asm volatile("ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\t"
+                             "s_waitcnt lgkmcnt(0)"
+                             : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3])
+                             : "v"(at ^ (d4 * 16)), "v"(at ^ (d4 * 16 + 16)), "v"(at ^ (d4 * 16 + 32)), "v"(at ^ (d4 * 16 + 48))
+                             : "memory");
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int r = u * 16 + 4 * q + (m16 >> 2);
-                f.half[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4 *)(st + L::kHalf + r * L::kRowBytes + (((2 * dt + ((m16 & 3) >> 1)) ^ L::swz(r)) * 16) + (m16 & 1) * 8));
-            }
-            return f.v;
-        };
-        // Where rows see different positions (or a page is missing), a value that one of them does not see may be an infinity or a NaN.  Single
-        // tokens see the same positions in all their rows, and what lies outside those was read from one of them.
-        bool rare = false;
-        if (masked && (holes || sr.n > 1)) {
-            uint32_t seen = 0;
+                for (int x = 0; x < 4; ++x) v[x] = widen_e4m3x8(w[x][0], w[x][1]);
+            } else {
+                const int r = 4 * q + (m16 >> 2);
+                const uint32_t at = (uint32_t)(uintptr_t)(LdsPtr)st + L::kHalf + r * L::kRowBytes + ((((m16 & 3) >> 1) ^ L::swz(r)) * 16) + (m16 & 1) * 8;
+                static_assert(E4M3 || L::swz(16) == 0, "positions 16 apart lie at the same chunk");
+                u32x2 w[8];
+                asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\tds_read_b64_tr_b16 %2, %9\n\t"
+                             "ds_read_b64_tr_b16 %3, %9 offset:%12\n\tds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7])
+                             : "v"(at ^ (d4 * 32)), "v"(at ^ (d4 * 32 + 32)), "v"(at ^ (d4 * 32 + 64)), "v"(at ^ (d4 * 32 + 96)), "n"(16 * L::kRowBytes)
+                             : "memory");
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const u32x4 w = __builtin_bit_cast(u32x4, frag(dt));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) seen = gather_nonfinite(seen, w[e]);
-            }
-            bool bad = any_nonfinite(seen);
-            if (E4M3) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bad |= !(fabsf(vs[e >> 2][e & 3]) < __builtin_inff());
-            }
-            rare = __ballot(bad) != 0;
-        }
-        if (!rare) {
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                if (E4M3) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) pv[n][e] *= vs[e >> 2][e & 3];
-                }
-                pf[n] = pack_bf16x8(pv[n]);
+                for (int x = 0; x < 4; ++x) v[x] = __builtin_bit_cast(bf16x8, u32x4{w[2 * x][0], w[2 * x][1], w[2 * x + 1][0], w[2 * x + 1][1]});
             }
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const bf16x8 v = frag(dt);
+            for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int n = 0; n < NR; ++n) acc[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[n], acc[n][dt], 0, 0, 0);
-            }
-        } else {
-            bf16x8 see[NR];
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                float one[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    one[e] = pv[n][e] == 0.f ? 0.f : 1.f;       // (a NaN counts as seen)
-                    if (E4M3) {
-                        const float sc = vs[e >> 2][e & 3];
-                        pv[n][e] = fabsf(sc) < __builtin_inff() ? pv[n][e] * sc : 0.f;
-                    }
-                }
-                pf[n] = pack_bf16x8(pv[n]);
-                see[n] = pack_bf16x8(one);
-            }
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                bf16x8 v = frag(dt), fine, up, down;
-                if (E4M3) {     // a scale that is not finite makes NaN of its row
-                    u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!(fabsf(vs[e >> 2][e & 3]) < __builtin_inff())) w[e >> 1] |= 0x7fc0u << (16 * (e & 1));
-                    v = __builtin_bit_cast(bf16x8, w);
-                }
-                split_nonfinite(v, fine, up, down);
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-                    const f32x4 ups = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, see[n], none, 0, 0, 0);
-                    const f32x4 downs = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, see[n], none, 0, 0, 0);
-                    acc[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fine, pf[n], acc[n][dt], 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[n][dt][e] += (ups[e] > 0.f ? __builtin_inff() : 0.f) + (downs[e] > 0.f ? kNegInf : 0.f);
-                }
-            }
+                for (int n = 0; n < NR; ++n) acc[n][d4 + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[x], pf[n], acc[n][d4 + x], 0, 0, 0);
         }
         slot = slot == L::kRing - 1 ? 0 : slot + 1;
     }
 
+    if (rare) {
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+            const int t = wave + i * kFewWaves, pos0 = lo + t * kFewTile;
+            const bool holes = __ballot(pages[t * 4 + ((lane & 31) >> 3)] < 0) != 0;
+            if (!holes && pos0 >= all_lo && pos0 + kFewTile - 1 <= all_hi) continue;
+            for (int j = max(pos0, begin); j < min(pos0 + kFewTile, end); ++j) {
+                const int page = pages[(j - lo) >> 3];
+                if (page < 0) continue;
+                const int64_t at = (((int64_t)page * Hkv + h) << shift) + (j & ((1 << shift) - 1));
+                const float sc = E4M3 ? a.kv.v_scales[at] : 1.f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t d = at * D + 16 * dt + 4 * q + e;
+                        const float v = E4M3 ? sc * __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)a.kv.v)[d], 0) : bf16_bits_to_f32(((const uint16_t *)a.kv.v)[d]);
+                        const bool bad = !(fabsf(v) < __builtin_inff());
+#pragma unroll
+                        for (int n = 0; n < NR; ++n)
+                            if (bad && j >= see_lo[n] && j <= see_hi[n]) acc[n][dt][e] += v;
+                    }
+            }
+        }
+    }
     // ---- the wavefronts' results meet in LDS (the ring's place; no copy is in flight any more)
     constexpr int kStride = D + 4;
     float *so = (float *)lds;                                             // [wave][16 NR][kStride]
