@@ -215,6 +215,10 @@ int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_h
         set_error("%s: q_heads must be a multiple of kv_heads and at most 1024 (got %d, %d)", who, q_heads, a.kv.kv_heads);
         return QARL_ERR_UNSUPPORTED;
     }
+    if ((int64_t)T * (q_heads / a.kv.kv_heads) > 0x7fff0000LL) {
+        set_error("%s: %d tokens of %d query heads per cached one exceed the row index", who, T, q_heads / a.kv.kv_heads);
+        return QARL_ERR_UNSUPPORTED;
+    }
     if (T == 0 || S == 0) return QARL_OK;
     if (!q_bf16 || !out || !kv_lens || !q_offsets || (!block_table && table_width > 0)) return bad_arg(who, "null pointer");
     if (max_q_len == 0) return bad_arg(who, "max_q_len must be positive where there are tokens");

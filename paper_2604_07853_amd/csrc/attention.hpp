@@ -45,7 +45,7 @@ struct AttnParts {
 struct SeqRange {
     int row_lo, n;        // first query row, queries
     int kv;               // cached positions, as the caller gives them: query i stands at kv - n + i
-    int64_t cap;          // positions from here on do not exist
+    int cap;              // positions from here on do not exist
 };
 
 __device__ __forceinline__ SeqRange seq_range(const AttnArgs &a, int s)
@@ -56,7 +56,7 @@ __device__ __forceinline__ SeqRange seq_range(const AttnArgs &a, int s)
     r.n = max(0, hi - lo);
     r.kv = max(0, a.kv_lens[s]);
     const int64_t table = (int64_t)a.table_width << a.kv.page_shift;
-    r.cap = min((int64_t)min(r.kv, a.max_kv_len), table);
+    r.cap = (int)min((int64_t)min(r.kv, a.max_kv_len), table);
     return r;
 }
 
@@ -64,7 +64,7 @@ __device__ __forceinline__ SeqRange seq_range(const AttnArgs &a, int s)
 __device__ __forceinline__ void visible_range(const AttnArgs &a, const SeqRange &s, int i0, int i1, int &begin, int &end)
 {
     const int64_t p0 = (int64_t)s.kv - s.n + i0, p1 = (int64_t)s.kv - s.n + i1;
-    const int64_t e = min(p1 + 1, s.cap);
+    const int64_t e = min(p1 + 1, (int64_t)s.cap);
     const int64_t b = a.window > 0 ? max((int64_t)0, p0 - a.window + 1) : 0;
     end = (int)max((int64_t)0, e);
     begin = (int)min(b, (int64_t)end);
@@ -74,8 +74,16 @@ __device__ __forceinline__ void visible_range(const AttnArgs &a, const SeqRange 
 __device__ __forceinline__ void row_bounds(const AttnArgs &a, const SeqRange &s, int i, int &lo, int &hi)
 {
     const int64_t p = (int64_t)s.kv - s.n + i;
-    hi = (int)min(p, s.cap - 1);
+    hi = (int)min(p, (int64_t)s.cap - 1);
     lo = a.window > 0 ? (int)max((int64_t)0, p - a.window + 1) : 0;
+}
+
+// max(lo, min(pos, hi)) for lo <= hi
+__device__ __forceinline__ int clamp_pos(int pos, int lo, int hi)
+{
+    int r;
+    asm("v_med3_i32 %0, %1, %2, %3" : "=v"(r) : "v"(pos), "v"(lo), "v"(hi));
+    return r;
 }
 
 // A word of bf16 pairs (of four e4m3 codes) with zeros for infinities and NaN (NaN)
@@ -90,15 +98,16 @@ __device__ __forceinline__ uint32_t only_finite_e4m3(uint32_t w)
     return w & ~((bad - (bad >> 7)) | bad);
 }
 
-// Eight fp32 -> bf16, nearest even (two per instruction)
-__device__ __forceinline__ bf16x8 pack_bf16x8(const float (&p)[8])
+// fp32 -> bf16, nearest even, two per instruction
+__device__ __forceinline__ uint32_t pack2_bf16(float x, float y)
 {
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-    u32x4 o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p[2 * i], p[2 * i + 1]}), bf16x2));
-    return __builtin_bit_cast(bf16x8, o);
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+}
+__device__ __forceinline__ bf16x8 pack_bf16x8(const float (&p)[8])
+{
+    return __builtin_bit_cast(bf16x8, u32x4{pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]), pack2_bf16(p[4], p[5]), pack2_bf16(p[6], p[7])});
 }
 
 // Eight e4m3 codes -> bf16 (exact; checked for all 256 codes on gfx950)
@@ -119,10 +128,7 @@ __device__ __forceinline__ void store_out4(const AttnArgs &a, int64_t row, int D
     if (a.out_f32) {
         *(f32x4 *)((float *)a.out + row * D + d) = v;
     } else {
-        u32x2 o;
-        o[0] = (uint32_t)f32_to_bf16_hw(v[0]) | (uint32_t)f32_to_bf16_hw(v[1]) << 16;
-        o[1] = (uint32_t)f32_to_bf16_hw(v[2]) | (uint32_t)f32_to_bf16_hw(v[3]) << 16;
-        *(u32x2 *)((uint16_t *)a.out + row * D + d) = o;
+        *(u32x2 *)((uint16_t *)a.out + row * D + d) = u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
     }
 }
 
