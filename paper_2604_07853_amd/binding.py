@@ -431,30 +431,36 @@ def qarl_tbpo_objective(lp_current, lp_old, lp_sampler, seq_offsets, advantage, 
     return out
 
 
+# Calls of a few microseconds on the GPU are bound by the host: the checks below read each property of a tensor once.
+_BF16, _F32, _U8, _I32, _I64 = torch.bfloat16, torch.float32, torch.uint8, torch.int32, torch.int64
+_raw_stream = torch._C._cuda_getCurrentRawStream        # handle of torch's current stream on a device
+
+
 def _dtype_code(t):
-    return QARL_OUT_F32 if t.dtype == torch.float32 else QARL_OUT_BF16
+    return QARL_OUT_F32 if t.dtype is _F32 else QARL_OUT_BF16
 
 
-def _rows(t, name, dtypes, shape):
-    """(pointer, stride) of a matrix whose rows are contiguous; (None, 0) for None."""
-    if t is None:
-        return None, 0
-    if not t.is_cuda or t.dtype not in dtypes or t.shape != shape or (shape[0] and shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be %s on the GPU, of type %s, with contiguous rows (got %s, %s)"
-                         % (name, list(shape), " or ".join(map(str, dtypes)), list(t.shape), t.dtype))
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+def _wrong(t, name, what):
+    raise ValueError("%s must be %s on the GPU (got %s %s on %s)" % (name, what, list(t.shape), t.dtype, t.device))
+
+
+def _rows(t, name, dtype, shape):
+    """(pointer, stride) of a matrix whose rows are contiguous."""
+    stride, last = t.stride() if t.dim() == 2 else (0, 0)
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or (last != 1 and shape[1] > 1 and shape[0]):
+        _wrong(t, name, "%s %s with contiguous rows" % (list(shape), dtype))
+    return t.data_ptr(), stride if shape[0] > 1 else max(stride, shape[1])
 
 
 def _flat(t, name, dtype, shape):
-    """Pointer of a contiguous tensor; None for None."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError("%s must be %s on the GPU, contiguous, of type %s (got %s, %s)" % (name, list(shape), dtype, list(t.shape), t.dtype))
+    """Pointer of a contiguous tensor."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        _wrong(t, name, "contiguous %s %s" % (list(shape), dtype))
     return t.data_ptr()
 
 
-_BF16, _STREAM = (torch.bfloat16,), (torch.bfloat16, torch.float32)
+def _ws(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def qarl_add_rmsnorm(x, weight, eps, residual=None, residual_out=None, y=None, codes=None, scales=None, quantize=False, via_bf16=False):
@@ -469,20 +475,25 @@ def qarl_add_rmsnorm(x, weight, eps, residual=None, residual_out=None, y=None, c
         codes = torch.empty((rows, K), dtype=torch.uint8, device=dev)
     if codes is not None and scales is None:
         scales = torch.empty((rows,), dtype=torch.float32, device=dev)
+    if codes is None and scales is not None:
+        raise ValueError("codes and scales go together")
     if y is None and codes is None:
         y = torch.empty((rows, K), dtype=torch.bfloat16, device=dev)
-    if residual is not None and residual_out.dtype != residual.dtype:
-        raise ValueError("residual and residual_out have different types")
     shape = (rows, K)
     xp, xs = _rows(x, "x", _BF16, shape)
-    rp, rs = _rows(residual, "residual", _STREAM, shape)
-    op, os_ = _rows(residual_out, "residual_out", _STREAM, shape)
-    yp, ys = _rows(y, "y", _BF16, shape)
-    st = residual_out if residual_out is not None else residual
-    _check(lib().qarl_add_rmsnorm(xp, xs, rp, rs, _flat(weight, "weight", torch.bfloat16, (K,)), rows, K, eps,
-                                  QARL_OUT_BF16 if st is None else _dtype_code(st), op, os_, yp, ys,
-                                  _flat(codes, "codes", torch.uint8, shape), _flat(scales, "scales", torch.float32, (rows,)),
-                                  int(via_bf16), torch.cuda.current_stream().cuda_stream))
+    rp = rs = op = os_ = yp = ys = cp = sp = None
+    code = QARL_OUT_BF16
+    if residual_out is not None:
+        code, dt = (QARL_OUT_F32, _F32) if residual_out.dtype is _F32 else (QARL_OUT_BF16, _BF16)
+        op, os_ = _rows(residual_out, "residual_out", dt, shape)
+        if residual is not None:
+            rp, rs = _rows(residual, "residual", dt, shape)
+    if y is not None:
+        yp, ys = _rows(y, "y", _BF16, shape)
+    if codes is not None:
+        cp, sp = _flat(codes, "codes", _U8, shape), _flat(scales, "scales", _F32, (rows,))
+    _check(lib().qarl_add_rmsnorm(xp, xs, rp, rs or 0, _flat(weight, "weight", _BF16, (K,)), rows, K, eps, code, op, os_ or 0, yp, ys or 0, cp, sp,
+                                  via_bf16, _raw_stream(x.get_device())))
     return dict(y=y, codes=codes, scales=scales, residual=residual_out)
 
 
@@ -502,17 +513,18 @@ def qarl_add_rmsnorm_backward(dy, h, weight, eps, dh=None, dx=None, dw=None, wan
         dw = torch.empty((K,), dtype=torch.float32 if dw_dtype == QARL_OUT_F32 else torch.bfloat16, device=dev)
     if dw is not None and ws is None:
         ws = torch.empty((lib().qarl_add_rmsnorm_backward_workspace_bytes(rows, K),), dtype=torch.uint8, device=dev)
-    same = (h.dtype,)
+    dt = _F32 if h.dtype is _F32 else _BF16
     yp, ys = _rows(dy, "dy", _BF16, shape)
-    hp, hs = _rows(h, "h", _STREAM, shape)
-    gp, gs = _rows(dh, "dh", same, shape)
-    xp, xs = _rows(dx, "dx", same, shape)
-    if dw is not None and dw.dtype not in _STREAM:
-        raise ValueError("dw must be bf16 or fp32 (got %s)" % dw.dtype)
-    _check(lib().qarl_add_rmsnorm_backward(yp, ys, hp, hs, gp, gs, _flat(weight, "weight", torch.bfloat16, (K,)), rows, K, eps,
-                                           _dtype_code(h), xp, xs, None if dw is None else _flat(dw, "dw", dw.dtype, (K,)),
-                                           QARL_OUT_F32 if dw is None else _dtype_code(dw), None if ws is None else ws.data_ptr(),
-                                           0 if ws is None else ws.numel() * ws.element_size(), torch.cuda.current_stream().cuda_stream))
+    hp, hs = _rows(h, "h", dt, shape)
+    gp, gs = (None, 0) if dh is None else _rows(dh, "dh", dt, shape)
+    xp, xs = _rows(dx, "dx", dt, shape)
+    wp, wcode = None, QARL_OUT_F32
+    if dw is not None:
+        wcode = QARL_OUT_F32 if dw.dtype is _F32 else QARL_OUT_BF16
+        wp = _flat(dw, "dw", _F32 if dw.dtype is _F32 else _BF16, (K,))
+    wsp, wsn = _ws(ws)
+    _check(lib().qarl_add_rmsnorm_backward(yp, ys, hp, hs, gp, gs, _flat(weight, "weight", _BF16, (K,)), rows, K, eps, _dtype_code(h), xp, xs,
+                                           wp, wcode, wsp, wsn, _raw_stream(h.get_device())))
     return dict(dx=dx, dw=dw)
 
 
@@ -535,6 +547,7 @@ class KVCache:
         self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.desc = qarl_kv_cache(fmt, self.num_pages, self.page_size, self.kv_heads, self.head_dim, k.data_ptr(), v.data_ptr(),
                                   k_scales.data_ptr() if fmt == QARL_KV_E4M3 else None, v_scales.data_ptr() if fmt == QARL_KV_E4M3 else None)
+        self.ref = C.byref(self.desc)
 
     @staticmethod
     def empty(fmt, num_pages, page_size, kv_heads, head_dim, device="cuda"):
@@ -548,24 +561,27 @@ class KVCache:
 
 def _heads(t, name, shape):
     """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose heads are contiguous."""
-    if not t.is_cuda or t.dtype != torch.bfloat16 or t.shape != shape or t.stride(2) != 1:
-        raise ValueError("%s must be bf16 %s on the GPU with contiguous heads (got %s, %s)" % (name, list(shape), list(t.shape), t.dtype))
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    token, head, last = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.shape != shape or t.dtype is not _BF16 or not t.is_cuda or last != 1:
+        _wrong(t, name, "%s %s with contiguous heads" % (list(shape), _BF16))
+    return t.data_ptr(), token, head
 
 
 def _table(t, S):
-    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != S or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("block_table must be int32 [%d, pages] on the GPU with contiguous rows (got %s, %s)" % (S, list(t.shape), t.dtype))
-    return t.data_ptr(), t.stride(0) if S > 1 else t.shape[1], t.shape[1]
+    stride, last = t.stride() if t.dim() == 2 else (0, 0)
+    width = t.shape[-1]
+    if t.shape != (S, width) or t.dtype is not _I32 or not t.is_cuda or (last != 1 and width > 1):
+        _wrong(t, "block_table", "[%d, pages] %s with contiguous rows" % (S, _I32))
+    return t.data_ptr(), stride if S > 1 else width, width
 
 
 def qarl_kv_cache_write(cache, k, v, slots):
     """Writes k, v [T, kv_heads, head_dim] (bf16, any token and head stride) into the slots [T] (int64) of the cache; see include/qarl.h."""
-    shape = (slots.numel(), cache.kv_heads, cache.head_dim)
+    T = slots.numel()
+    shape = (T, cache.kv_heads, cache.head_dim)
     kp, kt, kh = _heads(k, "k", shape)
     vp, vt, vh = _heads(v, "v", shape)
-    _check(lib().qarl_kv_cache_write(C.byref(cache.desc), kp, kt, kh, vp, vt, vh, shape[0],
-                                     _flat(slots, "slots", torch.int64, (shape[0],)), torch.cuda.current_stream().cuda_stream))
+    _check(lib().qarl_kv_cache_write(cache.ref, kp, kt, kh, vp, vt, vh, T, _flat(slots, "slots", _I64, (T,)), _raw_stream(k.get_device())))
 
 
 def qarl_kv_cache_read(cache, block_table, offsets, total, out=None):
@@ -577,14 +593,13 @@ def qarl_kv_cache_read(cache, block_table, offsets, total, out=None):
     k, v = out
     S = offsets.numel() - 1
     tp, ts, tw = _table(block_table, S)
-    _check(lib().qarl_kv_cache_read(C.byref(cache.desc), tp, ts, tw, _flat(offsets, "offsets", torch.int32, (S + 1,)), S, total,
-                                    _flat(k, "k", torch.bfloat16, shape), _flat(v, "v", torch.bfloat16, shape),
-                                    torch.cuda.current_stream().cuda_stream))
+    _check(lib().qarl_kv_cache_read(cache.ref, tp, ts, tw, _flat(offsets, "offsets", _I32, (S + 1,)), S, total, _flat(k, "k", _BF16, shape),
+                                    _flat(v, "v", _BF16, shape), _raw_stream(k.get_device())))
     return k, v
 
 
 def qarl_paged_attention_workspace_bytes(cache, T, q_heads, S, max_q_len, max_kv_len):
-    return lib().qarl_paged_attention_workspace_bytes(C.byref(cache.desc), T, q_heads, S, max_q_len, max_kv_len)
+    return lib().qarl_paged_attention_workspace_bytes(cache.ref, T, q_heads, S, max_q_len, max_kv_len)
 
 
 def qarl_paged_attention(query, cache, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, scale=None, window=0, out=None,
@@ -597,20 +612,19 @@ def qarl_paged_attention(query, cache, block_table, kv_lens, q_offsets, max_q_le
     S = kv_lens.numel()
     if out is None:
         out = torch.empty(shape, dtype=torch.float32 if out_dtype == QARL_OUT_F32 else torch.bfloat16, device=dev)
-    elif out.dtype not in _STREAM:
-        raise ValueError("out must be bf16 or fp32 (got %s)" % out.dtype)
     if lse is None and want_lse:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
     qp, qt, qh = _heads(query, "query", shape)
     tp, ts, tw = _table(block_table, S)
-    L, desc = lib(), C.byref(cache.desc)
+    L, ref = lib(), cache.ref
     if ws is None:
-        need = L.qarl_paged_attention_workspace_bytes(desc, T, Hq, S, max_q_len, max_kv_len)
+        need = L.qarl_paged_attention_workspace_bytes(ref, T, Hq, S, max_q_len, max_kv_len)
         if need:
-            ws = torch.empty((need,), dtype=torch.uint8, device=dev)
-    _check(L.qarl_paged_attention(qp, qt, qh, T, Hq, desc, tp, ts, tw, _flat(kv_lens, "kv_lens", torch.int32, (S,)),
-                                  _flat(q_offsets, "q_offsets", torch.int32, (S + 1,)), S, max_q_len, max_kv_len,
-                                  D ** -0.5 if scale is None else scale, window, _flat(out, "out", out.dtype, shape), _dtype_code(out),
-                                  _flat(lse, "lse", torch.float32, (T, Hq)), None if ws is None else ws.data_ptr(),
-                                  0 if ws is None else ws.numel() * ws.element_size(), torch.cuda.current_stream().cuda_stream))
+            ws = torch.empty((need,), dtype=_U8, device=dev)
+    wsp, wsn = _ws(ws)
+    f32 = out.dtype is _F32
+    _check(L.qarl_paged_attention(qp, qt, qh, T, Hq, ref, tp, ts, tw, _flat(kv_lens, "kv_lens", _I32, (S,)), _flat(q_offsets, "q_offsets", _I32, (S + 1,)),
+                                  S, max_q_len, max_kv_len, D ** -0.5 if scale is None else scale, window, _flat(out, "out", _F32 if f32 else _BF16, shape),
+                                  QARL_OUT_F32 if f32 else QARL_OUT_BF16, None if lse is None else _flat(lse, "lse", _F32, (T, Hq)), wsp, wsn,
+                                  _raw_stream(query.get_device())))
     return dict(out=out, lse=lse)

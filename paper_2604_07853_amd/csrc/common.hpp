@@ -203,6 +203,19 @@ __device__ __forceinline__ void bf16x8_to_f32(u32x4 v, float (&t)[8])
     }
 }
 
+// Accesses that bypass the caches (NT) or not
+template <bool NT, typename T>
+__device__ __forceinline__ T load_as(const void *p)
+{
+    return NT ? __builtin_nontemporal_load((const T *)p) : *(const T *)p;
+}
+template <bool NT, typename T>
+__device__ __forceinline__ void store_as(void *p, T v)
+{
+    if (NT) __builtin_nontemporal_store(v, (T *)p);
+    else *(T *)p = v;
+}
+
 // Eight fp32 values -> bf16, round to nearest even
 __device__ __forceinline__ u32x4 f32_to_bf16x8(const float (&t)[8])
 {
