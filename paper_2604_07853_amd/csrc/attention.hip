@@ -5,7 +5,12 @@ namespace qarl {
 
 // Sequences with at most 64 rows per cached head go to the kernel whose wavefronts share a sequence's positions, others to the one whose wavefronts
 // share its rows.  Both cut a cache into pieces where there are not enough (sequence, head, row block)s to fill the 256 CUs; partial results cost
-// 2 D fp32 per row and piece, so pieces are not shorter than that is worth.
+// 2 D fp32 per row and piece.
+//   Few rows: the lengths are not known here, so about four pieces per CU at the longest one; pieces of 512 positions or more.  Measured with 512 / 1024 /
+//   2048 / 4096 pieces wanted (us): 256 sequences of 4096 bf16 362 / 362 / 379 / 396, 16 of 4096 32 / 34 / 34 / 34, 256 of up to 18432 e4m3
+//   456 / 456 / 456 / 447; a single one of 18432 with 128 / 256 / 512 positions at least 23.9 / 19.6 / 18.4.
+//   Many rows: a workgroup per CU; beyond 192 blocks a cut costs more than it fills (1 x 2048 over 16384, 256 blocks: 626 whole, 658 in two;
+//   64 blocks: 307 estimated whole, 91 in four, 107 in eight; 160 blocks: 155 whole, 144 in four; 176 blocks: 448 whole, 403 in six).
 static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_q_len, int max_kv_len, int window)
 {
     AttnPlan p = {};
@@ -18,22 +23,21 @@ static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_
     if (!all_few && T > (int64_t)(S - 1) * most + 16 * p.few_nr / G) p.few_nr = 0;
     p.tile = !all_few;
     int64_t len = max_kv_len > 0 ? max_kv_len : 1;
-    const auto cut = [](int64_t length, int64_t items, int64_t wanted, int64_t least, int64_t unit, int64_t most_len, int &chunk, int &splits) {
-        int64_t n = (wanted + items - 1) / items;
-        n = min(n, (length + least - 1) / least);
-        n = n < 1 ? 1 : n;
-        int64_t c = ((length + n - 1) / n + unit - 1) / unit * unit;
-        c = min(max(c, least), most_len);
-        chunk = (int)c;
-        splits = (int)((length + c - 1) / c);
-    };
     if (window > 0) len = min(len, (int64_t)window + most + kManyTile);
-    if (p.few_nr) cut(len, (int64_t)S * kv_heads, 1024, 512, 128, 8192, p.few_chunk, p.few_splits);
+    // (the room for partial results goes by n, not by the pieces that the rounded length gives: it must not grow when a window shortens len)
+    const auto cut = [len, &p](int64_t n, int64_t unit, int64_t most_len, int &chunk, int &splits) {
+        n = max(min(n, (len + 511) / 512), (int64_t)1);
+        chunk = (int)min(((len + n - 1) / n + unit - 1) / unit * unit, most_len);
+        splits = (int)((len + chunk - 1) / chunk);
+        p.splits = max(p.splits, max((int)n, splits));
+    };
+    if (p.few_nr) cut((1024 + (int64_t)S * kv_heads - 1) / ((int64_t)S * kv_heads), 128, 8192, p.few_chunk, p.few_splits);
     if (p.tile) {
-        p.tile_blocks = (int)((T * G + kManyRows - 1) / kManyRows + min((int64_t)S, (int64_t)T));
-        cut(len, (int64_t)p.tile_blocks * kv_heads, 512, 512, 64, (int64_t)1 << 30, p.tile_chunk, p.tile_splits);
+        p.tile_blocks = (int)((T * G + kManyRows - 1) / kManyRows + min((int64_t)S, (int64_t)T));      // a bound
+        const bool even = T == (int64_t)S * most;
+        const int64_t blocks = kv_heads * (even ? S * ((most * G + kManyRows - 1) / kManyRows) : T * G / kManyRows + S / 2 + 1);
+        cut(blocks <= 128 ? 256 / blocks : blocks <= 192 ? 4 : 1, 64, (int64_t)1 << 30, p.tile_chunk, p.tile_splits);
     }
-    p.splits = p.few_splits > p.tile_splits ? p.few_splits : p.tile_splits;
     if (p.splits <= 1) p.splits = 0;
     return p;
 }
@@ -42,10 +46,9 @@ static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 size_t attention_ws_bytes(int T, int q_heads, int kv_heads, int head_dim, int S, int max_q_len, int max_kv_len)
 {
-    // a window makes the caches shorter, never the number of pieces larger: a piece more for the rounding
     const AttnPlan p = attention_plan(T, q_heads, kv_heads, S, max_q_len, max_kv_len, 0);
     if (!p.splits) return 0;
-    const size_t rows = (size_t)T * q_heads, n = (size_t)p.splits + 1;
+    const size_t rows = (size_t)T * q_heads, n = (size_t)p.splits;
     return up256(n * rows * head_dim * 4) + up256(n * rows * 8) + up256(rows * 4);
 }
 

@@ -292,7 +292,6 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int p0 = pos0 + u * 32;
-                if (u == 1 && p0 >= hi) break;      // the last tile may end in its first half
                 // ---- Scores of the next step and values of the last one on the matrix cores, probabilities of this one on the vector units: kSlots
                 // products, each with its share of the softmax and the read of the fragment four products on.  (The fences keep it so: left to itself
                 // the compiler puts the products side by side, and matrix cores and vector units take turns: 386 us for eight prompts of 2048.)
@@ -339,6 +338,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
                 uint32_t pn[8];
                 float p[16], sum[2] = {0.f, 0.f};
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);      // 2 % over even terms: a wavefront that feeds the matrix cores goes first
 #pragma unroll
                 for (int i = 0; i < kSlots; ++i) {
                     if (i + kAhead < kSlots) frag[i + kAhead] = i & 1 ? v_frag(vb, (i + kAhead) >> 1) : k_frag(kb, (i + kAhead) >> 1);
@@ -357,6 +357,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                __builtin_amdgcn_s_setprio(0);
                 pn[7] = pack2(p[14], p[15], vs[3], 14);
                 asm volatile("" : "+v"(pn[7]));
                 l = fmaf(l, keep, sum[0] + (sum[1] + p[15]));
@@ -377,10 +378,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
             slot = slot1;
         }
         const int last = slot == 0 ? 2 : slot - 1;      // (tiles - 1) % 3
-        const uint32_t last_u = lo + tiles * kManyTile - 32 >= hi ? 0 : 64;
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i)
-            acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag((at_v + last * L::kHalf) ^ last_u, i), probs(i / DT), acc[i % DT], 0, 0, 0);
+            acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag((at_v + last * L::kHalf) ^ 64, i), probs(i / DT), acc[i % DT], 0, 0, 0);
         rare = *lds_flag != 0;
     }
     if (rare) {

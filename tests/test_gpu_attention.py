@@ -223,6 +223,20 @@ def test_same_results_every_time_and_in_a_graph(q):
         assert torch.equal(got[0], out) and torch.equal(got[1], lse)
 
 
+@pytest.mark.parametrize("n,S", [(1, 1), (1, 3), (3, 2), (70, 1), (70, 3)])
+def test_the_workspace_asked_for_is_enough(q, n, S):
+    """Behind the bytes that the query names nothing is written, whatever the window (it changes how a cache is cut)."""
+    m = make(q, "bf16", [(n, 4700 - 100 * s) for s in range(S)], 8, 2, 64, 16, 21)
+    for max_kv in (4700, 4701, 5000, 6143, 9000):
+        need = q.qarl_paged_attention_workspace_bytes(m["c"], m["T"], 8, S, n, max_kv)
+        ws = torch.full((need + 65536,), 0x5a, dtype=torch.uint8, device="cuda")
+        for window in (0, 1, 700, 1500, 2560, 4000, 4600):
+            got = call(q, m, max_kv=max_kv, window=window, ws=ws)
+            assert (ws[need:] == 0x5a).all(), (max_kv, window)
+            if max_kv in (4701, 9000) and window in (0, 2560):
+                check(m, got, window=window, rows=[0, n - 1])
+
+
 def test_offsets_past_32_bits(q):
     """A cache of more than 2^32 bytes: the last pages hold the sequence."""
     page, heads, dim = 1024, 8, 128
