@@ -1,0 +1,77 @@
+"""A decoder layer on the library's own kernels: what a rollout engine (a few tokens per call) and the learner's forward (whole prompts) run.
+
+    residual add + RMS norm -> q, k, v projection -> paged cache (written quantized or plain) -> attention over it -> o projection
+    -> residual add + RMS norm (its output also as the experts' e4m3 rows) -> router -> quantized experts
+
+The projections are the grouped GEMM with one expert.  Positions are the caller's: `rotate(q, k)`, called on the views of the
+new tokens' queries and keys before they are cached, applies what the model uses.  The router's logits are a plain library product.
+"""
+import torch
+
+from . import binding as q
+
+
+class DecoderLayer:
+    """norm1, norm2 bf16 [H]; qkv QWeight [1, (heads + 2 kv_heads) * head_dim, H]; o QWeight [1, H, heads * head_dim]; router bf16 [experts, H];
+    gate_up, down the experts' QWeights; cache a KVCache of this layer."""
+
+    def __init__(self, norm1, qkv, o, norm2, router, gate_up, down, cache, topk=8, eps=1e-6):
+        D = cache.head_dim
+        self.H, self.heads = o.N, o.K // D
+        if (qkv.E, qkv.N, qkv.K) != (1, (self.heads + 2 * cache.kv_heads) * D, self.H) or o.E != 1 or o.K != self.heads * D:
+            raise ValueError("qkv and o must be one matrix each, [(heads + 2 kv_heads) * head_dim, H] and [H, heads * head_dim] (got %s, %s)"
+                             % ((qkv.E, qkv.N, qkv.K), (o.E, o.N, o.K)))
+        if norm1.shape != (self.H,) or norm2.shape != (self.H,) or router.shape != (gate_up.E, self.H) or gate_up.K != self.H:
+            raise ValueError("norms must be [%d], router [%d, %d] and gate_up of K = %d" % (self.H, gate_up.E, self.H, self.H))
+        self.norm1, self.qkv, self.o, self.norm2, self.router = norm1, qkv, o, norm2, router
+        self.gu, self.dn, self.cache, self.topk, self.eps = gate_up, down, cache, topk, eps
+        self.e4m3_rows = gate_up.fmt in q.E4M3_ACT_FORMATS
+        self._moe = {}          # decode batches, up to 512 tokens: the experts' layer object (its buffers) by number of tokens
+        self._one = {}          # and the row offsets of a projection, [0, T]
+
+    def _project(self, W, x):
+        T = x.shape[0]
+        offsets = self._one.get(T)
+        if offsets is None:
+            offsets = torch.tensor([0, T], dtype=torch.int32, device=x.device)
+            if T <= 512:
+                self._one[T] = offsets
+        return q.qarl_qgemm_grouped(W, x, offsets, T)
+
+    def _experts(self, y, codes, scales):
+        T = y.shape[0]
+        logits = torch.matmul(y, self.router.t())
+        if codes is None:
+            moe = self._moe.get(T)
+            if moe is None:     # few tokens: one call, the experts' kernels read (and quantize) the bf16 rows themselves
+                moe = q.MoELayer(self.gu, self.dn, T, self.topk, q.QARL_PATH_DECODE if T <= 512 else q.QARL_PATH_PREFILL, y.device)
+                if T <= 512:
+                    self._moe[T] = moe
+            return moe.forward(y, logits)
+        r = q.qarl_moe_route(logits, self.topk)
+        M = T * self.topk
+        a = q.qarl_qgemm_grouped(self.gu, codes, r.offsets, M, row_map=r.tokens, x_scales=scales, epilogue=q.QARL_EPI_SILU_MUL, path=q.QARL_PATH_PREFILL)
+        aq, sa = q.qarl_quantize_rows_fp8(a)
+        return q.qarl_qgemm_grouped(self.dn, aq, r.offsets, M, x_scales=sa, epilogue=q.QARL_EPI_COMBINE, combine_w=r.w, sorted_pairs=r.pairs, T=T,
+                                    topk=self.topk, path=q.QARL_PATH_PREFILL)
+
+    def forward(self, x, residual, slots, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, window=0, rotate=None):
+        """x [T, H] bf16: what the layer before has computed; residual [T, H]: the residual stream so far (None in front of the first layer).  slots,
+        block_table, kv_lens, q_offsets, max_q_len, max_kv_len: as for qarl_kv_cache_write and qarl_paged_attention, kv_lens with the new tokens.
+        Returns (output, residual) for the next layer, whose first norm adds them.  Up to 512 tokens the output is the layer's own buffer, written
+        again by the next call with as many tokens."""
+        T, c = x.shape[0], self.cache
+        n1 = q.qarl_add_rmsnorm(x, self.norm1, self.eps, residual=residual)
+        residual = x if residual is None else n1["residual"]
+        heads = self._project(self.qkv, n1["y"]).view(T, self.heads + 2 * c.kv_heads, c.head_dim)
+        query, key, value = heads.split([self.heads, c.kv_heads, c.kv_heads], 1)
+        if rotate is not None:
+            query, key = rotate(query, key)
+        q.qarl_kv_cache_write(c, key, value, slots)
+        att = q.qarl_paged_attention(query, c, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, window=window)["out"]
+        out = self._project(self.o, att.view(T, self.heads * c.head_dim))
+        # whole prompts on e4m3 rows: the norm quantizes them on the way, to the bytes that the decode path makes of its bf16 rows
+        fused = self.e4m3_rows and T > 512
+        y = torch.empty_like(out)
+        n2 = q.qarl_add_rmsnorm(out, self.norm2, self.eps, residual=residual, y=y, quantize=fused, via_bf16=True)
+        return self._experts(y, n2["codes"], n2["scales"]), n2["residual"]
