@@ -110,6 +110,18 @@ def test_lengths_of_one_sequence(q, fmt, n, context):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_more_row_blocks_than_cus(q, fmt, dim):
+    """Several rounds of workgroups, 70 sequences (more than a wavefront looks up at once), every row of every block written."""
+    lens = [(1 + 37 * s % 130, 1 + 37 * s % 130 + 11 * s % 60) for s in range(66)] + [(700, 700), (3, 900), (520, 1000), (900, 901)]
+    m = make(q, fmt, lens, 16, 2, dim, 16, 31)
+    out = torch.full((m["T"], 16, dim), math.nan, dtype=torch.bfloat16, device="cuda")
+    got = call(q, m, out=out)
+    assert got["out"].isfinite().all() and got["lse"].isfinite().all()
+    check(m, got, rows=[0, 40, 129, 350, 519, 699, 899])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
 @pytest.mark.parametrize("window", [1, 2, 31, 64, 100, 1000])
 def test_window(q, fmt, window):
     m = make(q, fmt, [(1, 257), (1, 3), (40, 200), (90, 90), (3, 130)], 8, 2, 64, 16, window)
