@@ -9,8 +9,9 @@ namespace qarl {
 //   Few rows: the lengths are not known here, so about four pieces per CU at the longest one; pieces of 512 positions or more.  Measured with 512 / 1024 /
 //   2048 / 4096 pieces wanted (us): 256 sequences of 4096 bf16 362 / 362 / 379 / 396, 16 of 4096 32 / 34 / 34 / 34, 256 of up to 18432 e4m3
 //   456 / 456 / 456 / 447; a single one of 18432 with 128 / 256 / 512 positions at least 23.9 / 19.6 / 18.4.
-//   Many rows: a workgroup per CU; beyond 192 blocks a cut costs more than it fills (1 x 2048 over 16384, 256 blocks: 626 whole, 658 in two;
-//   64 blocks: 307 estimated whole, 91 in four, 107 in eight; 160 blocks: 155 whole, 144 in four; 176 blocks: 448 whole, 403 in six).
+//   Many rows: a workgroup per CU; beyond 128 blocks a cut costs what it fills (1 x 2048 over 16384, 256 blocks: 626 us whole, 658 in two; 512 over 8192, 64
+//   blocks: 244 whole, 92 in four, 107 in eight; 4 x 300 over 4000, 160 blocks: 133 whole, 158 in two, 151 in four; 2 x 700 over 12000, 176 blocks: 419
+//   whole, 450 in two, 393 in four).
 static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_q_len, int max_kv_len, int window)
 {
     AttnPlan p = {};
@@ -36,7 +37,7 @@ static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_
         p.tile_blocks = (int)((T * G + kManyRows - 1) / kManyRows + min((int64_t)S, (int64_t)T));      // a bound
         const bool even = T == (int64_t)S * most;
         const int64_t blocks = kv_heads * (even ? S * ((most * G + kManyRows - 1) / kManyRows) : T * G / kManyRows + S / 2 + 1);
-        cut(blocks <= 128 ? 256 / blocks : blocks <= 192 ? 4 : 1, 64, (int64_t)1 << 30, p.tile_chunk, p.tile_splits);
+        cut(blocks <= 128 ? 256 / blocks : 1, 64, (int64_t)1 << 30, p.tile_chunk, p.tile_splits);
     }
     if (p.splits <= 1) p.splits = 0;
     return p;
@@ -52,68 +53,91 @@ size_t attention_ws_bytes(int T, int q_heads, int kv_heads, int head_dim, int S,
     return up256(n * rows * head_dim * 4) + up256(n * rows * 8) + up256(rows * 4);
 }
 
-// out = sum over the pieces of 2^(m_i - m) O_i / sum of 2^(m_i - m) l_i, in a fixed order.  D / 4 lanes per row and group; kGroups groups of a workgroup
-// share a row's pieces where there are many (one group: 26.8 us for the 72 pieces of a single token over 18432 positions).
-template <int D, int kGroups>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, AttnParts parts)
+// out = sum over the pieces of 2^(m_i - m) O_i / sum of 2^(m_i - m) l_i, in a fixed order.  A unit of D / 4 lanes holds a row.  A workgroup looks through
+// `per` rows, lists those that are in pieces, and joins them: a row of up to kAlone pieces by one unit, a row of more by all of them together.  (A single
+// token over 18432 positions: 72 pieces took one unit 26.8 us and take eight 4.0.)
+constexpr int kAlone = 8, kJoinRows = 256;
+
+template <int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, AttnParts parts, int per)
 {
-    constexpr int kLanes = D / 4, kRows = 256 / kLanes / kGroups;
-    __shared__ f32x4 so[kGroups > 1 ? 256 : 1];
-    __shared__ float sm[kGroups > 1 ? 256 / kLanes : 1], sl[kGroups > 1 ? 256 / kLanes : 1];
-    const int unit = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4, group = unit % kGroups;
-    const int64_t row = (int64_t)blockIdx.x * kRows + unit / kGroups;
-    int n = 0;
-    if (row < parts.rows) {
+    constexpr int kLanes = D / 4, kUnits = 256 / kLanes;
+    __shared__ f32x4 so[256];
+    __shared__ float sm[kUnits], sl[kUnits];
+    __shared__ int list[2][kJoinRows], listed[2];       // rows of few pieces, of many: row - row0, pieces << 16
+    const int unit = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+    const int64_t row0 = (int64_t)blockIdx.x * per;
+    if (threadIdx.x < 2) listed[threadIdx.x] = 0;
+    __syncthreads();
+    if ((int)threadIdx.x < per && row0 + threadIdx.x < parts.rows) {
+        const int64_t row = row0 + threadIdx.x;
         const int t = (int)(row / a.q_heads);
-        if (t >= a.q_offsets[0] && t < a.q_offsets[a.S]) n = min(parts.count[row], parts.splits);    // (none: a row of no sequence)
+        const int n = t >= a.q_offsets[0] && t < a.q_offsets[a.S] ? min(parts.count[row], parts.splits) : 0;    // (none: a row of no sequence)
+        if (n > 1) list[n > kAlone][atomicAdd(&listed[n > kAlone], 1)] = (int)threadIdx.x | n << 16;            // (one: written where it was computed)
     }
-    if (n <= 1) n = 0;                                           // written where it was computed
-    float top = kNegInf, sum = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
+    float top, sum;
+    f32x4 o;
+    const auto gather = [&](int64_t row, int n, int from, int step) {
+        top = kNegInf;
 #pragma unroll 4
-    for (int i = group; i < n; i += kGroups) top = fmaxf(top, parts.ml[((int64_t)i * parts.rows + row) * 2]);
-    const float tb = top == kNegInf ? 0.f : top;
+        for (int i = from; i < n; i += step) top = fmaxf(top, parts.ml[((int64_t)i * parts.rows + row) * 2]);
+        const float tb = top == kNegInf ? 0.f : top;
+        sum = 0.f;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int i = group; i < n; i += kGroups) {
-        const int64_t at = (int64_t)i * parts.rows + row;
-        const float f = __builtin_amdgcn_exp2f(parts.ml[at * 2] - tb);
-        sum += f * parts.ml[at * 2 + 1];
-        o += *(const f32x4 *)(parts.o + at * D + d) * f;
+        for (int i = from; i < n; i += step) {
+            const int64_t at = (int64_t)i * parts.rows + row;
+            const float f = __builtin_amdgcn_exp2f(parts.ml[at * 2] - tb);
+            sum += f * parts.ml[at * 2 + 1];
+            o += *(const f32x4 *)(parts.o + at * D + d) * f;
+        }
+    };
+    const auto finish = [&](int64_t row) {
+        store_out4(a, row, D, d, o * inverse_sum(sum));
+        if (d == 0 && a.lse) a.lse[row] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    };
+    for (int i = unit; i < listed[0]; i += kUnits) {
+        const int64_t row = row0 + (list[0][i] & 0xffff);
+        gather(row, list[0][i] >> 16, 0, 1);
+        finish(row);
     }
-    if (kGroups > 1) {
+    for (int i = 0; i < listed[1]; ++i) {
+        const int64_t row = row0 + (list[1][i] & 0xffff);
+        gather(row, list[1][i] >> 16, unit, kUnits);
         so[threadIdx.x] = o;
         if (d == 0) {
             sm[unit] = top;
             sl[unit] = sum;
         }
         __syncthreads();
-        if (group != 0) return;
-        for (int g = 0; g < kGroups; ++g) top = fmaxf(top, sm[unit + g]);
-        const float all = top == kNegInf ? 0.f : top;
-        sum = 0.f;
-        o = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int g = 0; g < kGroups; ++g) {
-            const float f = __builtin_amdgcn_exp2f(sm[unit + g] - all);
-            sum += f * sl[unit + g];
-            o += so[threadIdx.x + g * kLanes] * f;
+        if (unit == 0) {
+            for (int g = 0; g < kUnits; ++g) top = fmaxf(top, sm[g]);
+            const float all = top == kNegInf ? 0.f : top;
+            sum = 0.f;
+            o = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int g = 0; g < kUnits; ++g) {
+                const float f = __builtin_amdgcn_exp2f(sm[g] - all);
+                sum += f * sl[g];
+                o += so[threadIdx.x + g * kLanes] * f;
+            }
+            finish(row);
         }
+        __syncthreads();
     }
-    if (n == 0) return;
-    store_out4(a, row, D, d, o * inverse_sum(sum));
-    if (d == 0 && a.lse) a.lse[row] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int D>
 static int launch_join(const AttnArgs &a, const AttnParts &parts, hipStream_t s)
 {
-    const bool many = parts.splits > 8;
-    const int64_t per = many ? 256 / (D / 4) / 8 : 256 / (D / 4), blocks = (parts.rows + per - 1) / per;
+    // rows per workgroup: about as many workgroups as the chip holds at a time
+    const int per = (int)max((int64_t)1, min((int64_t)kJoinRows, parts.rows / 2048));
+    const int64_t blocks = (parts.rows + per - 1) / per;
     if (blocks > 0x7fffffffLL) {
         set_error("qarl_paged_attention: %lld rows exceed the grid limit", (long long)parts.rows);
         return QARL_ERR_UNSUPPORTED;
     }
-    if (many) attention_join_kernel<D, 8><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, parts);
-    else attention_join_kernel<D, 1><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, parts);
+    attention_join_kernel<D><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, parts, per);
     return check_hip(hipGetLastError(), "attention_join_kernel");
 }
 

@@ -109,6 +109,15 @@ def test_lengths_of_one_sequence(q, fmt, n, context):
     check(m, call(q, m), rows=sorted({0, 1, n // 3, n // 2, n - 2, n - 1} & set(range(n))))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_pieces_of_every_number_in_one_call(q, dim):
+    """Rows of one piece, of a few and of many (single tokens over caches of all lengths), alone and beside long chunks with thousands of rows."""
+    tokens = [(1, n) for n in (1, 300, 512, 513, 1100, 1600, 2047, 3000, 4100, 4609, 5200, 6000)]
+    for seqs in (tokens, tokens + [(600, 700), (1, 5900), (300, 1400), (2, 4800)]):
+        m = make(q, "bf16", seqs, 16, 2, dim, 16, 41)
+        check(m, call(q, m), rows=[0, 1, 299, 599])
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "fp8"])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_more_row_blocks_than_cus(q, fmt, dim):
