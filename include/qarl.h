@@ -368,11 +368,13 @@ int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, i
  *   q_bf16 [T][q_heads] rows at q_token_stride and q_head_stride (elements, multiples of 8), 16-byte aligned; out [T][q_heads][head_dim],
  *   bf16 or fp32 (out_dtype).  Cached values at positions that a query does not see never reach its result, whatever their bits.
  *   max_q_len, max_kv_len: host bounds of n and of kv_lens[s]; cached positions from max_kv_len on, and from
- *   table_width * page_size on, are cut off; rows past max_q_len of a sequence may be left unwritten.  Pages outside
+ *   table_width * page_size on, are cut off; a sequence of more than max_q_len queries may be left unwritten.  Pages outside
  *   [0, num_pages) hold nothing: their positions are not seen.
- *   ws: qarl_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (0 for calls that are not split along the cache).
- * A sequence's cache is split where there are few rows; a row's result depends on its sequence and on (T, S, max_q_len, max_kv_len),
- * not on timing.  Supported: q_heads % kv_heads == 0, q_heads <= 1024.  T == 0 or S == 0 is a no-op. */
+ *   ws: qarl_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (0 for calls that are not split along the cache); what it
+ *   holds before the call does not matter.
+ * A sequence's cache is split where there are few rows; a row's result depends on its sequence and on (T, S, the heads, max_q_len,
+ * max_kv_len, window), not on timing.  Supported: q_heads % kv_heads == 0, q_heads <= 1024, T * (q_heads / kv_heads) <= 2^31 - 2^16.
+ * T == 0 or S == 0 is a no-op. */
 size_t qarl_paged_attention_workspace_bytes(const qarl_kv_cache *cache, int T, int q_heads, int S, int max_q_len,
                                             int max_kv_len);
 int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_head_stride, int T, int q_heads,

@@ -1,16 +1,19 @@
 // Attention of many query rows per sequence (prompts, chunks of prompts) over the paged cache.
-// Bound by the matrix cores and exp2.  A workgroup takes a block of 256 rows of one cached head (rows are (query, head of the group)) and runs over the
-// cache in tiles of 64 positions, which its four wavefronts share through rings of three tiles in LDS.
+// Bound by what the SIMDs issue, products and softmax together.  A workgroup takes a block of 256 rows of one cached head (rows are (query, head of the
+// group)) and runs over the cache in tiles of 64 positions, which its eight wavefronts share through rings of three tiles in LDS.
 //
-// S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 matrix instructions: a wavefront owns 64 rows, two sets of 32, so that every fragment read from LDS
-// feeds two instructions (with 32 rows the LDS reads alone would take as long as the products: 1.1 us per 256 rows and tile).  Lane (n = lane & 31,
+// S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 matrix instructions: a wavefront owns 32 rows, two wavefronts share a SIMD.  (64 rows would halve the LDS
+// reads, but spill 600 registers beside a second wavefront, and without one move 300 a tile between the two register files.)  Lane (n = lane & 31,
 // half = lane >> 5) holds row n's scores at positions 8 (i / 4) + 4 half + i % 4, i = 0 .. 15, of 32 positions: the maximum and the sum of a row are
 // in-lane but for one exchange between the halves, and registers 8 t .. 8 t + 7, packed to bf16, are the B operand of step t of the second product as
 // they are (contraction order {4 half + 0..3, 8 + 4 half + 0..3} of 16 positions).  V^T in that order lies in LDS: a tile's values are transposed on their way.
 //
-// That takes the registers of a whole SIMD (one wavefront each), so what overlaps is one wavefront's own work: step s (32 positions) computes the scores
-// of step s + 1 and adds the values of step s - 1 on the matrix cores while the vector units turn the scores of step s into probabilities; none of the three
-// waits for another.
+// A wavefront's own work overlaps: step s (32 positions) computes the scores of step s + 1 and adds the values of step s - 1 on the matrix cores while the
+// vector units turn the scores of step s into probabilities; none of the three waits for another.
+//
+// Measured, 32 query heads on 4 cached ones of 128: eight prompts of 2048 bf16 347 us (275 GFLOP, 792 TFLOP/s), 4 x 2048 over 16384 cached positions
+// 2266 us (1031 TFLOP/s); 28 heads on 4, 12 chunks of mixed lengths over an e4m3 cache 335 us (776 TFLOP/s).  A tile takes 4040-4160 cycles, 2048 of
+// them products; a block 7 us more to start and end.
 #include "attention.hpp"
 
 namespace qarl {
