@@ -225,9 +225,9 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             l[n] += sum;
         }
         // ---- values.  Where rows see different positions (or a page is missing), a value that one of them does not see may be an infinity or a NaN,
-        // and its product with the probability 0 a NaN: such values become zeros in LDS, and the rows that see them get them in the end.  Single tokens
-        // see the same positions in all their rows, and what lies outside those was read from one of them.
-        if (masked && (holes || sr.n > 1)) {
+        // and its product with the probability 0 a NaN: such values become zeros in LDS, and the rows that see them get them in the end.  (For single
+        // tokens too: what lies outside the positions that they see was read from the nearest of those.)
+        if (masked) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < L::kHalf / 1024; ++i) {

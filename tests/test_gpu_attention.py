@@ -273,3 +273,26 @@ def test_offsets_past_32_bits(q):
         a = q.qarl_paged_attention(query[:n], big, torch.tensor([[pages - 2, pages - 1]], dtype=torch.int32, device="cuda"), *args)["out"]
         b = q.qarl_paged_attention(query[:n], small, torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), *args)["out"]
         assert torch.equal(a, b) and a.isfinite().all() and a.abs().sum() > 0
+
+
+@pytest.mark.parametrize("n", [1, 3, 70])
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_visible_infinities_at_the_ends_reach_the_result(q, fmt, n):
+    """An infinity at the last or the first position that a query sees gives infinities, however much of its tile lies outside (a product with the
+    probability 0 of a position that is not there would give NaN)."""
+    window = 50
+    for total in (n, n + 17, n + 95):
+        for first in (False, True):
+            m = make(q, fmt, [(n, total)], 8, 2, 64, 16, total + 5)
+            at = max(0, total - window) if first else total - 1             # the last query's ends
+            page, off = int(m["table"][0, at // 16]), at % 16
+            v, scales = m["host"][1]
+            if fmt == "fp8":
+                v[page, :, off] = 0x38 + (torch.arange(64) % 2 * 128).to(torch.uint8)        # 1 and -1 in turn
+                scales[page, :, off] = math.inf
+                m["c"].v_scales.copy_(scales)
+            else:
+                v[page, :, off] = torch.where(torch.arange(64) % 2 == 0, math.inf, -math.inf).to(torch.bfloat16)
+            m["c"].v.copy_(v)
+            got = call(q, m, window=window)["out"][n - 1].double().cpu()
+            assert torch.equal(got, torch.where(torch.arange(64) % 2 == 0, math.inf, -math.inf).double().expand(8, 64)), (total, first)
