@@ -374,7 +374,7 @@ int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, i
  *   holds before the call does not matter.
  * A sequence's cache is split where there are few rows; a row's result depends on its sequence and on (T, S, the heads, max_q_len,
  * max_kv_len, window), not on timing.  Supported: q_heads % kv_heads == 0, q_heads <= 1024, T * (q_heads / kv_heads) <= 2^31 - 2^16.
- * T == 0 or S == 0 is a no-op. */
+ * max_kv_len <= 2^28, |scale| <= 1e38.  T == 0 or S == 0 is a no-op. */
 size_t qarl_paged_attention_workspace_bytes(const qarl_kv_cache *cache, int T, int q_heads, int S, int max_q_len,
                                             int max_kv_len);
 int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_head_stride, int T, int q_heads,

@@ -210,13 +210,17 @@ int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_h
     if (rc || (rc = check_dtype(who, "out_dtype", out_dtype))) return rc;
     if (T < 0 || S < 0 || q_heads <= 0 || max_q_len < 0 || max_kv_len < 0 || table_width < 0 || window < 0)
         return bad_arg(who, "T, S, max_q_len, max_kv_len, table_width and window must not be negative, q_heads must be positive");
-    if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return bad_arg(who, "scale must be finite");
+    if (!(scale >= -1.0e38f && scale <= 1.0e38f)) return bad_arg(who, "scale must be finite, at most 1e38 in size");     // (times log2 e it is still finite)
     if (q_heads % a.kv.kv_heads != 0 || q_heads > 1024) {
         set_error("%s: q_heads must be a multiple of kv_heads and at most 1024 (got %d, %d)", who, q_heads, a.kv.kv_heads);
         return QARL_ERR_UNSUPPORTED;
     }
     if ((int64_t)T * (q_heads / a.kv.kv_heads) > 0x7fff0000LL) {
         set_error("%s: %d tokens of %d query heads per cached one exceed the row index", who, T, q_heads / a.kv.kv_heads);
+        return QARL_ERR_UNSUPPORTED;
+    }
+    if (max_kv_len > 1 << 28) {
+        set_error("%s: max_kv_len is at most 2^28 (got %d)", who, max_kv_len);
         return QARL_ERR_UNSUPPORTED;
     }
     if (T == 0 || S == 0) return QARL_OK;

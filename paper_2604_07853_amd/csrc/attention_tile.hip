@@ -119,10 +119,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
         for (int ks = 0; ks < KS; ++ks) {
             u32x4 w = *(const u32x4 *)(qp + 16 * ks + 8 * half);
             if (a.scale < 0.f) w ^= 0x80008000u;        // scores go by the scale's size: the running maximum wants it positive
+            if (a.scale == 0.f) {                       // zeros, but for infinities and NaN
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] ^= only_finite_bf16(w[e]);
+            }
             qf[ks] = __builtin_bit_cast(bf16x8, w);
         }
     }
-    const float c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f), stale = kStale / c2;
+    // (8 / c2 has to be finite)
+    const float c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f), stale = kStale / c2;
     // positions [all_lo, all_hi] are seen by all rows of the wavefront, [any_lo, any_hi] by one at least (a wavefront without rows: none)
     int all_lo, all_hi, any_lo, any_hi;
     {

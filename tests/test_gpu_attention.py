@@ -296,3 +296,15 @@ def test_visible_infinities_at_the_ends_reach_the_result(q, fmt, n):
             m["c"].v.copy_(v)
             got = call(q, m, window=window)["out"][n - 1].double().cpu()
             assert torch.equal(got, torch.where(torch.arange(64) % 2 == 0, math.inf, -math.inf).double().expand(8, 64)), (total, first)
+
+
+@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("scale", [0.0, 1e-36, -1e-33])
+def test_scales_of_small_size(q, n, scale):
+    """Scores that are large before they are scaled (16 coordinates of up to 2^60 each): the scale counts as it is, however small."""
+    m = make(q, "bf16", [(n, n + 30)], 4, 2, 64, 16, 3)
+    m["query"] = (m["query"].float() * 2.0 ** 55).to(torch.bfloat16)
+    k = (m["host"][0][0].float() * 2.0 ** 55).to(torch.bfloat16)
+    m["host"][0] = (k, None)
+    m["c"].k.copy_(k)
+    check(m, call(q, m, scale=scale), scale=scale)

@@ -122,6 +122,15 @@ def test_attention(q):
     assert fn(*_attention(q, T=0, q=None).values()) == q.QARL_OK and fn(*_attention(q, S=0, q=None).values()) == q.QARL_OK
 
 
+def test_attention_refuses_scales_and_lengths_that_overflow_inside(q):
+    """scale * log2 e has to stay finite; a row's number of pieces has to fit the join's lists."""
+    fn = q.lib().qarl_paged_attention
+    for scale in (3e38, -3e38, 2.5e38):
+        _refused(q, q.QARL_ERR_INVALID_ARG, "finite", fn, _attention(q, scale=scale))
+    _refused(q, q.QARL_ERR_UNSUPPORTED, "2^28", fn, _attention(q, mkv=(1 << 28) + 1))
+    assert fn(*_attention(q, T=0, q=None, mkv=1 << 28, scale=1e38).values()) == q.QARL_OK
+
+
 def test_binding_refuses_tensors_of_other_shapes_and_types(q):
     """On the host, before a pointer is taken: CPU tensors, other types, other sizes."""
     x, w = torch.zeros((4, 64), dtype=torch.bfloat16), torch.ones(64, dtype=torch.bfloat16)
