@@ -308,3 +308,13 @@ def test_scales_of_small_size(q, n, scale):
     m["host"][0] = (k, None)
     m["c"].k.copy_(k)
     check(m, call(q, m, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("n,total,window", [(9, 700, 0), (33, 33, 0), (300, 300, 0), (300, 700, 40), (290, 1000, 200), (257, 400, 1)])
+def test_wavefronts_that_see_different_tiles(q, fmt, n, total, window):
+    """One query head per cached one and eight: wavefronts without rows, behind the diagonal, in front of a window's start, in one piece and in several."""
+    for heads, S in ((2, 1), (16, 1), (2, 40)):
+        m = make(q, fmt, [(n, total)] * S if S == 1 else [(n - s % 3, total - s) if total - s >= n else (n, total) for s in range(S)], heads, 2, 64, 16, n)
+        got = call(q, m, window=window)
+        check(dict(m, seqs=m["seqs"][:2]), got, window=window, rows=sorted({r for r in (0, 1, 31, 32, 33, 63, 64, 127, 128, n - 34, n - 33, n - 2, n - 1) if r >= 0}))
