@@ -6,12 +6,26 @@ namespace qarl {
 // Sequences with at most 64 rows per cached head go to the kernel whose wavefronts share a sequence's positions, others to the one whose wavefronts
 // share its rows.  Both cut a cache into pieces where there are not enough (sequence, head, row block)s to fill the 256 CUs; partial results cost
 // 2 D fp32 per row and piece.
-//   Few rows: the lengths are not known here, so about four pieces per CU at the longest one; pieces of 512 positions or more.  Measured with 512 / 1024 /
-//   2048 / 4096 pieces wanted (us): 256 sequences of 4096 bf16 362 / 362 / 379 / 396, 16 of 4096 32 / 34 / 34 / 34, 256 of up to 18432 e4m3
-//   456 / 456 / 456 / 447; a single one of 18432 with 128 / 256 / 512 positions at least 23.9 / 19.6 / 18.4.
+//   Few rows: pieces of 512 positions or more (a single sequence of 18432 with 256 / 384 / 512 at least: 20.7 / 16.2 / 16.0 us).  One workgroup runs on a CU.
+//   From 256 (sequence, head)s on about four pieces per CU at the longest length, for the lengths are not known here: 64 ragged sequences of up to
+//   18000, 4 heads, 8 / 32 / 64 rows with one piece 232 / 253 / 327, with four 211 / 232 / 290 (of equal lengths 8000, 32 / 64 rows, the other way:
+//   190 / 204 against 207 / 244).  Below that few_pieces(): 16 of 4096, 8 / 64 rows 34 / 46 instead of 40 / 69 with four pieces per CU; 48 of 12000, 64 rows,
+//   with 256 / 512 / 768 / 1024 wanted 282 / 300 / 257 / 282.
 //   Many rows: a workgroup per CU; beyond 128 blocks a cut costs what it fills (1 x 2048 over 16384, 256 blocks: 626 us whole, 658 in two; 512 over 8192, 64
 //   blocks: 244 whole, 92 in four, 107 in eight; 4 x 300 over 4000, 160 blocks: 133 whole, 158 in two, 151 in four; 2 x 700 over 12000, 176 blocks: 419
 //   whole, 450 in two, 393 in four).
+// Pieces per (sequence, head) so that they fill 256 CUs one to four times, at the least cost for sequences of the longest length: positions, and for
+// each piece's start and end as much as `extra` of them take.  (Shorter lengths never give more pieces: the room for partial results relies on it.)
+static int64_t few_pieces(int64_t units, int64_t len, int64_t extra)
+{
+    int64_t best = 1, times = 1;
+    for (int64_t r = 1; r <= 4; ++r) {
+        const int64_t n = 256 * r / units;
+        if (r == 1 || r * (len + extra * n) * best < times * (len + extra * best) * n) best = n, times = r;
+    }
+    return best;
+}
+
 static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_q_len, int max_kv_len, int window)
 {
     AttnPlan p = {};
@@ -32,7 +46,10 @@ static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_
         splits = (int)((len + chunk - 1) / chunk);
         p.splits = max(p.splits, max((int)n, splits));
     };
-    if (p.few_nr) cut((1024 + (int64_t)S * kv_heads - 1) / ((int64_t)S * kv_heads), 128, 8192, p.few_chunk, p.few_splits);
+    if (p.few_nr) {
+        const int64_t units = (int64_t)S * kv_heads;
+        cut(units >= 256 ? (1024 + units - 1) / units : few_pieces(units, len, p.few_nr == 4 ? 512 : 256), 128, 8192, p.few_chunk, p.few_splits);
+    }
     if (p.tile) {
         p.tile_blocks = (int)((T * G + kManyRows - 1) / kManyRows + min((int64_t)S, (int64_t)T));      // a bound
         const bool even = T == (int64_t)S * most;
@@ -64,7 +81,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, AttnPar
     constexpr int kLanes = D / 4, kUnits = 256 / kLanes;
     __shared__ f32x4 so[256];
     __shared__ float sm[kUnits], sl[kUnits];
-    __shared__ int list[2][kJoinRows], listed[2];       // rows of few pieces, of many: row - row0, pieces << 16
+    __shared__ unsigned list[2][kJoinRows];             // rows of few pieces, of many: row - row0, pieces << 16
+    __shared__ int listed[2];
     const int unit = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
     const int64_t row0 = (int64_t)blockIdx.x * per;
     if (threadIdx.x < 2) listed[threadIdx.x] = 0;
@@ -73,7 +91,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, AttnPar
         const int64_t row = row0 + threadIdx.x;
         const int t = (int)(row / a.q_heads);
         const int n = t >= a.q_offsets[0] && t < a.q_offsets[a.S] ? min(parts.count[row], parts.splits) : 0;    // (none: a row of no sequence)
-        if (n > 1) list[n > kAlone][atomicAdd(&listed[n > kAlone], 1)] = (int)threadIdx.x | n << 16;            // (one: written where it was computed)
+        if (n > 1) list[n > kAlone][atomicAdd(&listed[n > kAlone], 1)] = threadIdx.x | (unsigned)n << 16;           // (one: written where it was computed)
     }
     __syncthreads();
     float top, sum;
@@ -99,12 +117,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, AttnPar
     };
     for (int i = unit; i < listed[0]; i += kUnits) {
         const int64_t row = row0 + (list[0][i] & 0xffff);
-        gather(row, list[0][i] >> 16, 0, 1);
+        gather(row, (int)(list[0][i] >> 16), 0, 1);
         finish(row);
     }
     for (int i = 0; i < listed[1]; ++i) {
         const int64_t row = row0 + (list[1][i] & 0xffff);
-        gather(row, list[1][i] >> 16, unit, kUnits);
+        gather(row, (int)(list[1][i] >> 16), unit, kUnits);
         so[threadIdx.x] = o;
         if (d == 0) {
             sm[unit] = top;
