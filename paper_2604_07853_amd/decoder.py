@@ -26,7 +26,8 @@ class DecoderLayer:
         self.norm1, self.qkv, self.o, self.norm2, self.router = norm1, qkv, o, norm2, router
         self.gu, self.dn, self.cache, self.topk, self.eps = gate_up, down, cache, topk, eps
         self.e4m3_rows = gate_up.fmt in q.E4M3_ACT_FORMATS
-        self._moe = {}          # decode batches, up to 512 tokens: the experts' layer object (its buffers) by number of tokens
+        self._moe = {}          # decode batches, up to 512 tokens: the experts' layer object by number of tokens,
+        self._room = None       # all on the buffers of the largest (a server meets every number of them, and a captured step keeps its addresses)
         self._one = {}          # and the row offsets of a projection, [0, T]
 
     def _project(self, W, x):
@@ -46,6 +47,11 @@ class DecoderLayer:
             if moe is None:     # few tokens: one call, the experts' kernels read (and quantize) the bf16 rows themselves
                 moe = q.MoELayer(self.gu, self.dn, T, self.topk, q.QARL_PATH_DECODE if T <= 512 else q.QARL_PATH_PREFILL, y.device)
                 if T <= 512:
+                    if self._room is None:
+                        self._room = q.MoELayer(self.gu, self.dn, 512, self.topk, q.QARL_PATH_DECODE, y.device)
+                    moe.a, moe.out = self._room.a[: moe.M], self._room.out[:T]
+                    if moe.ws.numel() <= self._room.ws.numel():
+                        moe.ws = self._room.ws
                     self._moe[T] = moe
             return moe.forward(y, logits)
         r = q.qarl_moe_route(logits, self.topk)
@@ -59,7 +65,7 @@ class DecoderLayer:
         """x [T, H] bf16: what the layer before has computed; residual [T, H]: the residual stream so far (None in front of the first layer).  slots,
         block_table, kv_lens, q_offsets, max_q_len, max_kv_len: as for qarl_kv_cache_write and qarl_paged_attention, kv_lens with the new tokens.
         Returns (output, residual) for the next layer, whose first norm adds them.  Up to 512 tokens the output is the layer's own buffer, written
-        again by the next call with as many tokens."""
+        again by its next call of up to 512."""
         T, c = x.shape[0], self.cache
         n1 = q.qarl_add_rmsnorm(x, self.norm1, self.eps, residual=residual)
         residual = x if residual is None else n1["residual"]

@@ -104,3 +104,19 @@ def test_sizes_that_do_not_fit_are_refused(q):
     for bad in (dict(qkv=a.o), dict(norm1=a.norm1[:-1]), dict(router=a.router[:-1]), dict(cache=q.KVCache.empty(q.QARL_KV_BF16, 8, PAGE, KV * 2, D))):
         with pytest.raises(ValueError):
             DecoderLayer(**dict(good, **bad))
+
+
+@pytest.mark.parametrize("fmt", ["QARL_W4A16_G128", "QARL_FP8_E4M3_CH"])
+def test_batches_of_every_size_share_one_set_of_buffers(q, fmt):
+    """A layer that meets many batch sizes holds the intermediates of one, and its results are those of a layer that has met no other."""
+    pages = 40
+    layer = layer_of(q, getattr(q, fmt), q.QARL_KV_BF16, pages)
+    for T in (5, 300, 1, 17, 512, 5):
+        x, p = synth.normal_bf16((T, H), 1.0, 40 + T).cuda(), plan([T], [0], pages)
+        out, stream = (t.clone() for t in layer.forward(x, None, **p))
+        fresh = layer_of(q, getattr(q, fmt), q.QARL_KV_BF16, pages)
+        want = fresh.forward(x, None, **p)
+        assert torch.equal(out, want[0]) and torch.equal(stream, want[1]), T
+    assert len(layer._moe) == 5
+    for name in ("a", "out"):
+        assert len({getattr(m, name).untyped_storage().data_ptr() for m in layer._moe.values()}) == 1
