@@ -564,7 +564,7 @@ def _heads(t, name, shape):
     token, head, last = t.stride() if t.dim() == 3 else (0, 0, 0)
     if t.shape != shape or t.dtype is not _BF16 or not t.is_cuda or last != 1:
         _wrong(t, name, "%s %s with contiguous heads" % (list(shape), _BF16))
-    return t.data_ptr(), token, head
+    return t.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0      # (the stride of a single one may be anything)
 
 
 def _table(t, S):

@@ -318,3 +318,17 @@ def test_wavefronts_that_see_different_tiles(q, fmt, n, total, window):
         m = make(q, fmt, [(n, total)] * S if S == 1 else [(n - s % 3, total - s) if total - s >= n else (n, total) for s in range(S)], heads, 2, 64, 16, n)
         got = call(q, m, window=window)
         check(dict(m, seqs=m["seqs"][:2]), got, window=window, rows=sorted({r for r in (0, 1, 31, 32, 33, 63, 64, 127, 128, n - 34, n - 33, n - 2, n - 1) if r >= 0}))
+
+
+def test_strides_of_single_tokens_and_heads_do_not_matter(q):
+    """A batch of one token, or one head, cut out of rows whose length is no multiple of eight."""
+    m = make(q, "bf16", [(1, 40)], 4, 1, 64, 16, 9)
+    wide = torch.zeros((2, 4 * 64 + 3), dtype=torch.bfloat16, device="cuda")
+    wide[0, :256] = m["query"][0, 1:5].reshape(-1).cuda()
+    view = wide.as_strided((1, 4, 64), (259, 64, 1))
+    args = (m["c"], m["table"].cuda(), m["kv_lens"].cuda(), m["offsets"].cuda(), 1, 40)
+    assert view.stride()[0] % 8 and torch.equal(q.qarl_paged_attention(view, *args)["out"], q.qarl_paged_attention(view.contiguous(), *args)["out"])
+    k = torch.randn((8, 64), device="cuda").to(torch.bfloat16).as_strided((8, 1, 64), (64, 3, 1))
+    before = m["c"].k.clone()
+    q.qarl_kv_cache_write(m["c"], k, k, torch.arange(8, device="cuda"))
+    assert torch.equal(m["c"].k[0, 0, :8], k[:, 0]) and torch.equal(m["c"].k[0, 0, 8:].view(torch.int16), before[0, 0, 8:].view(torch.int16))
