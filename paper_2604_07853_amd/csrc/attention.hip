@@ -3,17 +3,6 @@
 
 namespace qarl {
 
-// Sequences with at most 64 rows per cached head go to the kernel whose wavefronts share a sequence's positions, others to the one whose wavefronts
-// share its rows.  Both cut a cache into pieces where there are not enough (sequence, head, row block)s to fill the 256 CUs; partial results cost
-// 2 D fp32 per row and piece.
-//   Few rows: pieces of 512 positions or more (a single sequence of 18432 with 256 / 384 / 512 at least: 20.7 / 16.2 / 16.0 us).  One workgroup runs on a CU.
-//   From 256 (sequence, head)s on about four pieces per CU at the longest length, for the lengths are not known here: 64 ragged sequences of up to
-//   18000, 4 heads, 8 / 32 / 64 rows with one piece 232 / 253 / 327, with four 211 / 232 / 290 (of equal lengths 8000, 32 / 64 rows, the other way:
-//   190 / 204 against 207 / 244).  Below that few_pieces(): 16 of 4096, 8 / 64 rows 34 / 46 instead of 40 / 69 with four pieces per CU; 48 of 12000, 64 rows,
-//   with 256 / 512 / 768 / 1024 wanted 282 / 300 / 257 / 282.
-//   Many rows: a workgroup per CU; beyond 128 blocks a cut costs what it fills (1 x 2048 over 16384, 256 blocks: 626 us whole, 658 in two; 512 over 8192, 64
-//   blocks: 244 whole, 92 in four, 107 in eight; 4 x 300 over 4000, 160 blocks: 133 whole, 158 in two, 151 in four; 2 x 700 over 12000, 176 blocks: 419
-//   whole, 450 in two, 393 in four).
 // Pieces per (sequence, head) so that they fill 256 CUs one to four times, at the least cost for sequences of the longest length: positions, and for
 // each piece's start and end as much as `extra` of them take.  (Shorter lengths never give more pieces: the room for partial results relies on it.)
 static int64_t few_pieces(int64_t units, int64_t len, int64_t extra)
@@ -26,6 +15,18 @@ static int64_t few_pieces(int64_t units, int64_t len, int64_t extra)
     return best;
 }
 
+// Sequences with at most 64 rows per cached head go to the kernel whose wavefronts share a sequence's positions, others to the one whose wavefronts
+// share its rows.  Both cut a cache into pieces where there are not enough (sequence, head, row block)s to fill the 256 CUs; partial results cost
+// 2 D fp32 per row and piece.
+//   Few rows: pieces of 512 positions or more (a single sequence of 18432 with 256 / 384 / 512 at least: 20.7 / 16.2 / 16.0 us).  A CU holds one workgroup, or two
+//   whose rings are 64 KiB.
+//   From 256 (sequence, head)s on about four pieces per CU at the longest length, for the lengths are not known here: 64 ragged sequences of up to
+//   18000, 4 heads, 8 / 32 / 64 rows with one piece 232 / 253 / 327, with four 211 / 232 / 290 (of equal lengths 8000, 32 / 64 rows, the other way:
+//   190 / 204 against 207 / 244).  Below that few_pieces(): 16 of 4096, 8 / 64 rows 34 / 46 instead of 40 / 69 with four pieces per CU; 48 of 12000, 64 rows,
+//   with 256 / 512 / 768 / 1024 wanted 282 / 300 / 257 / 282.
+//   Many rows: a workgroup per CU; beyond 128 blocks a cut costs what it fills (1 x 2048 over 16384, 256 blocks: 626 us whole, 658 in two; 512 over 8192, 64
+//   blocks: 244 whole, 92 in four, 107 in eight; 4 x 300 over 4000, 160 blocks: 133 whole, 158 in two, 151 in four; 2 x 700 over 12000, 176 blocks: 419
+//   whole, 450 in two, 393 in four).
 static AttnPlan attention_plan(int T, int q_heads, int kv_heads, int S, int max_q_len, int max_kv_len, int window)
 {
     AttnPlan p = {};
