@@ -368,7 +368,7 @@ int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, i
  *   q_bf16 [T][q_heads] rows at q_token_stride and q_head_stride (elements, multiples of 8), 16-byte aligned; out [T][q_heads][head_dim],
  *   bf16 or fp32 (out_dtype).  Cached values at positions that a query does not see never reach its result, whatever their bits.
  *   max_q_len, max_kv_len: host bounds of n and of kv_lens[s]; cached positions from max_kv_len on, and from
- *   table_width * page_size on, are cut off; a sequence of more than max_q_len queries may be left unwritten.  Pages outside
+ *   table_width * page_size on, are cut off; the rows of a sequence of more than max_q_len queries are left as they are.  Pages outside
  *   [0, num_pages) hold nothing: their positions are not seen.
  *   ws: qarl_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (0 for calls that are not split along the cache); what it
  *   holds before the call does not matter.

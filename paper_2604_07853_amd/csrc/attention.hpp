@@ -8,7 +8,7 @@
 // A row block is a run of rows r = i * G + g of one cached head: query i of the sequence, head g of the G query heads that read that
 // cached head, so that a key or value read once serves all of them.
 #pragma once
-#include "common.hpp"
+#include "attention_split.hpp"
 
 namespace qarl {
 
@@ -19,20 +19,6 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kStale = 8.f;   // a running maximum may lag behind by this many powers of two before the sums are rescaled
 
-// How a call is split: each kernel takes the sequences whose row count (queries times G) lies on its side of few_rows, and cuts a
-// sequence's cache into pieces of `chunk` positions.
-struct AttnPlan {
-    int few_nr;        // the kernel for few rows: 16 * few_nr rows at a time; 0: not launched
-    int few_chunk, few_splits;
-    int tile;          // the kernel for many rows is launched
-    int tile_chunk, tile_splits, tile_blocks;   // tile_blocks: bound of the row blocks of one cached head
-    int splits;        // room for partial results per row (0: none)
-};
-
-constexpr int kFewTile = 32;      // positions a wavefront of the few-row kernel takes at a time
-constexpr int kManyTile = 64;     // positions of a tile of the many-row kernel
-constexpr int kManyWaves = 8, kManyRows = 256;
-
 // Partial results in the workspace: O [splits][T * q_heads][D], then (m, l) [splits][T * q_heads], then the number of pieces [T * q_heads]
 struct AttnParts {
     float *o;
@@ -41,42 +27,6 @@ struct AttnParts {
     int splits;
     int64_t rows;
 };
-
-struct SeqRange {
-    int row_lo, n;        // first query row, queries
-    int kv;               // cached positions, as the caller gives them: query i stands at kv - n + i
-    int cap;              // positions from here on do not exist
-};
-
-__device__ __forceinline__ SeqRange seq_range(const AttnArgs &a, int s)
-{
-    SeqRange r;
-    const int lo = max(0, min(a.T, a.q_offsets[s])), hi = max(0, min(a.T, a.q_offsets[s + 1]));
-    r.row_lo = lo;
-    r.n = max(0, hi - lo);
-    r.kv = max(0, a.kv_lens[s]);
-    const int64_t table = (int64_t)a.table_width << a.kv.page_shift;
-    r.cap = (int)min((int64_t)min(r.kv, a.max_kv_len), table);
-    return r;
-}
-
-// Positions [begin, end) that queries [i0, i1] see between them (none: begin == end)
-__device__ __forceinline__ void visible_range(const AttnArgs &a, const SeqRange &s, int i0, int i1, int &begin, int &end)
-{
-    const int64_t p0 = (int64_t)s.kv - s.n + i0, p1 = (int64_t)s.kv - s.n + i1;
-    const int64_t e = min(p1 + 1, (int64_t)s.cap);
-    const int64_t b = a.window > 0 ? max((int64_t)0, p0 - a.window + 1) : 0;
-    end = (int)max((int64_t)0, e);
-    begin = (int)min(b, (int64_t)end);
-}
-
-// What a row sees: positions lo <= j <= hi
-__device__ __forceinline__ void row_bounds(const AttnArgs &a, const SeqRange &s, int i, int &lo, int &hi)
-{
-    const int64_t p = (int64_t)s.kv - s.n + i;
-    hi = (int)min(p, (int64_t)s.cap - 1);
-    lo = a.window > 0 ? (int)max((int64_t)0, p - a.window + 1) : 0;
-}
 
 // max(lo, min(pos, hi)) for lo <= hi
 __device__ __forceinline__ int clamp_pos(int pos, int lo, int hi)

@@ -42,12 +42,17 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
     const unsigned sh = blockIdx.x - (unsigned)split * per_split;
     const int s = (int)(sh / (unsigned)Hkv), h = (int)(sh - (unsigned)s * (unsigned)Hkv);
     const SeqRange sr = seq_range(a, s);
+    if (over_long(a, sr)) {
+        if (split == 0 && parts.splits > 0) {
+            for (int64_t i = tid; i < (int64_t)sr.n * G; i += kFewThreads) parts.count[(sr.row_lo + i / G) * a.q_heads + h * G + i % G] = 0;
+        }
+        return;
+    }
     if (sr.n == 0 || (int64_t)sr.n * G > 16 * NR) return;
     const int R = sr.n * G;
     int begin, end;
     visible_range(a, sr, 0, sr.n - 1, begin, end);
-    const int base = begin & ~(kFewTile - 1);
-    const int pieces = max(1, (end - base + chunk - 1) / chunk);
+    const auto [base, pieces] = cut_range(begin, end, kFewTile, chunk);
     if (split >= pieces) return;
     const int lo = base + split * chunk, hi = min(end, lo + chunk);      // this piece; lo is a multiple of 32
     const int tiles = (hi - lo + kFewTile - 1) / kFewTile;               // (0 where nothing is visible)

@@ -92,10 +92,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
     if (s < 0) return;                                  // the grid is a bound
     const int row0 = block * kManyRows, in_block = min(kManyRows, sr.n * G - row0);
     const int i_first = (int)((unsigned)row0 / (unsigned)G), i_last = (int)((unsigned)(row0 + in_block - 1) / (unsigned)G);
+    if (over_long(a, sr)) {
+        if (split == 0 && parts.splits > 0) {
+            for (int r = row0 + tid; r < row0 + in_block; r += kManyThreads) {
+                const int i = (int)((unsigned)r / (unsigned)G);
+                parts.count[(int64_t)(sr.row_lo + i) * a.q_heads + (h * G + r - i * G)] = 0;
+            }
+        }
+        return;
+    }
     int begin, end;
     visible_range(a, sr, i_first, i_last, begin, end);
-    const int base = begin & ~(kManyTile - 1);
-    const int pieces = max(1, (end - base + chunk - 1) / chunk);
+    const auto [base, pieces] = cut_range(begin, end, kManyTile, chunk);
     if (split >= pieces) return;
     const int lo = base + split * chunk, hi = min(end, lo + chunk);
     const int tiles = (hi - lo + kManyTile - 1) / kManyTile;

@@ -332,3 +332,25 @@ def test_strides_of_single_tokens_and_heads_do_not_matter(q):
     before = m["c"].k.clone()
     q.qarl_kv_cache_write(m["c"], k, k, torch.arange(8, device="cuda"))
     assert torch.equal(m["c"].k[0, 0, :8], k[:, 0]) and torch.equal(m["c"].k[0, 0, 8:].view(torch.int16), before[0, 0, 8:].view(torch.int16))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("heads,max_q,window,seqs", [
+    (2, 65, 1, [(300, 300)]), (16, 4, 1, [(90, 700), (1, 40)]),                                 # a window's positions in more pieces than max_q_len lets expect
+    (16, 1, 0, [(1, 3000), (5, 4000), (1, 2500)]), (2, 1, 0, [(40, 3000), (1, 3000)]),          # single tokens
+    (2, 70, 0, [(70, 2000), (1, 3000), (200, 2500), (3, 50)]), (16, 70, 0, [(70, 2000), (1, 3000), (71, 2500), (2, 50)]),
+    (2, 70, 40, [(70, 2000), (500, 800), (1, 3000)]), (2, 40, 0, [(33, 900), (41, 900), (64, 64), (65, 70)])])
+def test_sequences_longer_than_the_bound_are_left_alone(q, fmt, heads, max_q, window, seqs):
+    """max_q_len is the caller's bound: a longer sequence's rows stay as they are, whatever the workspace held, and the others are right."""
+    m = make(q, fmt, seqs, heads, 2, 64, 16, 51)
+    max_kv = max(n for _, n in seqs)
+    ws = torch.full((q.qarl_paged_attention_workspace_bytes(m["c"], m["T"], heads, len(seqs), max_q, max_kv),), 1, dtype=torch.uint8, device="cuda")
+    out = torch.full((m["T"], heads, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((m["T"], heads), 9.0, device="cuda")
+    got = q.qarl_paged_attention(m["query"].cuda()[:, 1: 1 + heads], m["c"], m["table"].cuda(), m["kv_lens"].cuda(), m["offsets"].cuda(), max_q, max_kv,
+                                 window=window, out=out, lse=lse, ws=ws)
+    for s, (n, _) in enumerate(seqs):
+        lo = int(m["offsets"][s])
+        if n > max_q:
+            assert (out[lo: lo + n] == 9).all() and (lse[lo: lo + n] == 9).all(), s
+    check(dict(m, seqs=[(n if n <= max_q else 0, total) for n, total in seqs]), got, window=window)
