@@ -37,14 +37,15 @@ __host__ __device__ inline SeqRange seq_range(const AttnArgs &a, int s)
     return r;
 }
 
-// Positions [begin, end) that queries [i0, i1] see between them (none: begin == end)
+// Positions [begin, end) that queries [i0, i1] see between them.  None (a query in front of the first position, a window that starts behind the last one
+// there is): 0, 0, so that no tile is made of them; the tiles' reads stay within a range by its first and last position, which then do not exist.
 __host__ __device__ inline void visible_range(const AttnArgs &a, const SeqRange &s, int i0, int i1, int &begin, int &end)
 {
     const int64_t p0 = (int64_t)s.kv - s.n + i0, p1 = (int64_t)s.kv - s.n + i1;
     const int64_t e = min(p1 + 1, (int64_t)s.cap);
     const int64_t b = a.window > 0 ? max((int64_t)0, p0 - a.window + 1) : 0;
-    end = (int)max((int64_t)0, e);
-    begin = (int)min(b, (int64_t)end);
+    end = e > b ? (int)e : 0;
+    begin = e > b ? (int)b : 0;
 }
 
 // What a row sees: positions lo <= j <= hi

@@ -68,6 +68,8 @@ int main(int argc, char **argv)
                 int begin, end;
                 visible_range(a, r, (int)(row0 / G), (int)(last / G), begin, end);
                 const Pieces cut = cut_range(begin, end, unit, chunk);
+                if (begin >= end && end - cut.base > 0) broken = "tiles of positions that nobody sees";
+                if (end > a.max_kv_len || end > (a.table_width << a.kv.page_shift)) broken = "positions past the bounds";
                 if (cut.count > splits) broken = "more pieces than are launched";
                 if (cut.count > std::max(1, p.splits)) broken = "more pieces than there is room for";
             }

@@ -354,3 +354,21 @@ def test_sequences_longer_than_the_bound_are_left_alone(q, fmt, heads, max_q, wi
         if n > max_q:
             assert (out[lo: lo + n] == 9).all() and (lse[lo: lo + n] == 9).all(), s
     check(dict(m, seqs=[(n if n <= max_q else 0, total) for n, total in seqs]), got, window=window)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("n", [1, 3, 70, 300])
+def test_windows_that_start_behind_the_last_position_there_is(q, fmt, n):
+    """kv_lens past what the table holds (80 positions) or max_kv_len allows, and a window that starts there: zeros and lse -inf; rows whose window reaches
+    back before it see what is left."""
+    for total, window, max_kv in ((1000 + n, 10, 1000 + n), (81 + n + 20, 20, 81 + n + 20), (80 + n, 40, 80 + n), (n + 400, 30, 72), (n + 75, 30, 72)):
+        m = make(q, fmt, [(n, total), (2, 90)], 8, 2, 64, 16, n + 7)
+        m["table"] = m["table"][:, :5].contiguous()
+        got = call(q, m, max_kv=max_kv, window=window)
+        if max_kv >= 80:
+            check(m, got, window=window)
+        for i in range(n):
+            if total - n + i - window + 1 >= min(80, max_kv):
+                assert (got["out"][i] == 0).all() and (got["lse"][i] == -math.inf).all(), (total, window, i)
+            else:
+                assert got["out"][i].isfinite().all() and got["lse"][i].isfinite().all() and (got["out"][i] != 0).any(), (total, window, i)
