@@ -134,8 +134,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
             qf[ks] = __builtin_bit_cast(bf16x8, w);
         }
     }
-    // (8 / c2 has to be finite)
-    const float c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f), stale = kStale / c2;
+    // (scale 0: the scores are zeros, infinities or NaN already, and 0 times the maximum's start -inf would be a NaN; the lag has to be finite for the same start)
+    const float c2 = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e, stale = fminf(kStale / c2, 3e38f);
     // positions [all_lo, all_hi] are seen by all rows of the wavefront, [any_lo, any_hi] by one at least (a wavefront without rows: none)
     int all_lo, all_hi, any_lo, any_hi;
     {

@@ -372,3 +372,34 @@ def test_windows_that_start_behind_the_last_position_there_is(q, fmt, n):
                 assert (got["out"][i] == 0).all() and (got["lse"][i] == -math.inf).all(), (total, window, i)
             else:
                 assert got["out"][i].isfinite().all() and got["lse"][i].isfinite().all() and (got["out"][i] != 0).any(), (total, window, i)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("scale", [2e-38, -3e-38, 1e-39, -5e-40])
+def test_scales_below_the_smallest_normal_ones(q, fmt, n, scale):
+    """Scores of up to 2^126 before they are scaled: in both kernels the scale counts as it is.  Its product with log2 e is then a subnormal number, and so is
+    that with a key's scale (0.13 or more here): half a step of 2^-149 on each."""
+    m = make(q, fmt, [(n, n + 30)], 4, 2, 64, 16, 3)
+    if fmt == "bf16":
+        m["query"] = (m["query"].float() * 2.0 ** 60).to(torch.bfloat16)
+        k = (m["host"][0][0].float() * 2.0 ** 61).to(torch.bfloat16)
+        m["host"][0] = (k, None)
+        m["c"].k.copy_(k)
+    else:                                                   # codes of up to 448 and scales of about 0.005
+        m["query"] = (m["query"].float() * 2.0 ** 113).to(torch.bfloat16)
+        sc = m["host"][0][1] * 2.0 ** 7
+        m["host"][0] = (m["host"][0][0], sc)
+        m["c"].k_scales.copy_(sc)
+    got = call(q, m, scale=scale)
+    low = 2.0 ** -149 / abs(scale) * (1 if fmt == "bf16" else 8)
+    as_given = torch.tensor(scale, dtype=torch.float32).item()
+    for i in range(n):
+        k, ok = ref.cached(*m["host"][0], m["table"][0], n + 30, 16)
+        v, _ = ref.cached(*m["host"][1], m["table"][0], n + 30, 16)
+        o, e, mag, zerr = ref.attention(m["query"][i: i + 1, 1:5], k, v, ok, 31 + i, as_given, 0)
+        top = zerr[0] / ((64 + 8) * ref.F32)                # the scores' own size
+        err = zerr[0] + low * top
+        tol = mag[0] * (ref.HALF_BF16 + 2 * err[:, None] + 2.0 ** -19) + o[0].abs() * 1.01 * ref.HALF_BF16
+        assert ((got["out"][i].double().cpu() - o[0]).abs() <= tol).all(), (i, float(top.max()))
+        assert ((got["lse"][i].double().cpu() - e[0]).abs() <= err + 2.0 ** -19 * (1 + e[0].abs())).all(), (i, float(top.max()))
