@@ -440,27 +440,40 @@ def _dtype_code(t):
     return QARL_OUT_F32 if t.dtype is _F32 else QARL_OUT_BF16
 
 
-def _wrong(t, name, what):
-    raise ValueError("%s must be %s on the GPU (got %s %s on %s)" % (name, what, list(t.shape), t.dtype, t.device))
+def _wrong(t, name, what, gpu):
+    raise ValueError("%s must be %s on %s (got %s %s on %s)" % (name, what, "the GPU" if gpu < 0 else "cuda:%d" % gpu, list(t.shape), t.dtype, t.device))
 
 
-def _rows(t, name, dtype, shape):
+# Every tensor of a call lies on the GPU `gpu`, that of its first one (get_device() is -1 in host memory, which a kernel must not be handed).
+def _rows(t, name, dtype, shape, gpu):
     """(pointer, stride) of a matrix whose rows are contiguous."""
     stride, last = t.stride() if t.dim() == 2 else (0, 0)
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or (last != 1 and shape[1] > 1 and shape[0]):
-        _wrong(t, name, "%s %s with contiguous rows" % (list(shape), dtype))
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != gpu or gpu < 0 or (last != 1 and shape[1] > 1 and shape[0]):
+        _wrong(t, name, "%s %s with contiguous rows" % (list(shape), dtype), gpu)
     return t.data_ptr(), stride if shape[0] > 1 else max(stride, shape[1])
 
 
-def _flat(t, name, dtype, shape):
+def _flat(t, name, dtype, shape, gpu):
     """Pointer of a contiguous tensor."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        _wrong(t, name, "contiguous %s %s" % (list(shape), dtype))
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != gpu or gpu < 0 or not t.is_contiguous():
+        _wrong(t, name, "contiguous %s %s" % (list(shape), dtype), gpu)
     return t.data_ptr()
 
 
-def _ws(ws):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+def _ws(ws, gpu):
+    """(pointer, bytes) of a workspace."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != gpu or gpu < 0 or not ws.is_contiguous():
+        _wrong(ws, "ws", "contiguous", gpu)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _cache(cache, gpu):
+    """The descriptor of a cache."""
+    if cache.gpu != gpu or gpu < 0:
+        raise ValueError("the cache must be on %s (it is on %s)" % ("the GPU" if gpu < 0 else "cuda:%d" % gpu, cache.k.device))
+    return cache.ref
 
 
 def qarl_add_rmsnorm(x, weight, eps, residual=None, residual_out=None, y=None, codes=None, scales=None, quantize=False, via_bf16=False):
@@ -479,21 +492,21 @@ def qarl_add_rmsnorm(x, weight, eps, residual=None, residual_out=None, y=None, c
         raise ValueError("codes and scales go together")
     if y is None and codes is None:
         y = torch.empty((rows, K), dtype=torch.bfloat16, device=dev)
-    shape = (rows, K)
-    xp, xs = _rows(x, "x", _BF16, shape)
+    shape, gpu = (rows, K), x.get_device()
+    xp, xs = _rows(x, "x", _BF16, shape, gpu)
     rp = rs = op = os_ = yp = ys = cp = sp = None
     code = QARL_OUT_BF16
     if residual_out is not None:
         code, dt = (QARL_OUT_F32, _F32) if residual_out.dtype is _F32 else (QARL_OUT_BF16, _BF16)
-        op, os_ = _rows(residual_out, "residual_out", dt, shape)
+        op, os_ = _rows(residual_out, "residual_out", dt, shape, gpu)
         if residual is not None:
-            rp, rs = _rows(residual, "residual", dt, shape)
+            rp, rs = _rows(residual, "residual", dt, shape, gpu)
     if y is not None:
-        yp, ys = _rows(y, "y", _BF16, shape)
+        yp, ys = _rows(y, "y", _BF16, shape, gpu)
     if codes is not None:
-        cp, sp = _flat(codes, "codes", _U8, shape), _flat(scales, "scales", _F32, (rows,))
-    _check(lib().qarl_add_rmsnorm(xp, xs, rp, rs or 0, _flat(weight, "weight", _BF16, (K,)), rows, K, eps, code, op, os_ or 0, yp, ys or 0, cp, sp,
-                                  via_bf16, _raw_stream(x.get_device())))
+        cp, sp = _flat(codes, "codes", _U8, shape, gpu), _flat(scales, "scales", _F32, (rows,), gpu)
+    _check(lib().qarl_add_rmsnorm(xp, xs, rp, rs or 0, _flat(weight, "weight", _BF16, (K,), gpu), rows, K, eps, code, op, os_ or 0, yp, ys or 0, cp, sp,
+                                  via_bf16, _raw_stream(gpu)))
     return dict(y=y, codes=codes, scales=scales, residual=residual_out)
 
 
@@ -506,7 +519,7 @@ def qarl_add_rmsnorm_backward(dy, h, weight, eps, dh=None, dx=None, dw=None, wan
     the residual stream.  Allocates dx, dw (want_dw) and ws when not given.  Returns dict(dx, dw)."""
     rows, K = h.shape
     dev = h.device
-    shape = (rows, K)
+    shape, gpu = (rows, K), h.get_device()
     if dx is None:
         dx = torch.empty(shape, dtype=h.dtype, device=dev)
     if dw is None and want_dw:
@@ -514,17 +527,17 @@ def qarl_add_rmsnorm_backward(dy, h, weight, eps, dh=None, dx=None, dw=None, wan
     if dw is not None and ws is None:
         ws = torch.empty((lib().qarl_add_rmsnorm_backward_workspace_bytes(rows, K),), dtype=torch.uint8, device=dev)
     dt = _F32 if h.dtype is _F32 else _BF16
-    yp, ys = _rows(dy, "dy", _BF16, shape)
-    hp, hs = _rows(h, "h", dt, shape)
-    gp, gs = (None, 0) if dh is None else _rows(dh, "dh", dt, shape)
-    xp, xs = _rows(dx, "dx", dt, shape)
+    yp, ys = _rows(dy, "dy", _BF16, shape, gpu)
+    hp, hs = _rows(h, "h", dt, shape, gpu)
+    gp, gs = (None, 0) if dh is None else _rows(dh, "dh", dt, shape, gpu)
+    xp, xs = _rows(dx, "dx", dt, shape, gpu)
     wp, wcode = None, QARL_OUT_F32
     if dw is not None:
         wcode = QARL_OUT_F32 if dw.dtype is _F32 else QARL_OUT_BF16
-        wp = _flat(dw, "dw", _F32 if dw.dtype is _F32 else _BF16, (K,))
-    wsp, wsn = _ws(ws)
-    _check(lib().qarl_add_rmsnorm_backward(yp, ys, hp, hs, gp, gs, _flat(weight, "weight", _BF16, (K,)), rows, K, eps, _dtype_code(h), xp, xs,
-                                           wp, wcode, wsp, wsn, _raw_stream(h.get_device())))
+        wp = _flat(dw, "dw", _F32 if dw.dtype is _F32 else _BF16, (K,), gpu)
+    wsp, wsn = _ws(ws, gpu)
+    _check(lib().qarl_add_rmsnorm_backward(yp, ys, hp, hs, gp, gs, _flat(weight, "weight", _BF16, (K,), gpu), rows, K, eps, _dtype_code(h), xp, xs,
+                                           wp, wcode, wsp, wsn, _raw_stream(gpu)))
     return dict(dx=dx, dw=dw)
 
 
@@ -543,11 +556,14 @@ class KVCache:
             for t in (k_scales, v_scales):
                 if t is None or t.dtype != torch.float32 or t.shape != k.shape[:3] or not t.is_contiguous():
                     raise ValueError("k_scales and v_scales must be contiguous fp32 tensors %s" % list(k.shape[:3]))
+        if any(t.device != k.device for t in ((v, k_scales, v_scales) if fmt == QARL_KV_E4M3 else (v,))):
+            raise ValueError("the buffers of a cache must be on one device")
         self.fmt, self.k, self.v, self.k_scales, self.v_scales = fmt, k, v, k_scales, v_scales
         self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.desc = qarl_kv_cache(fmt, self.num_pages, self.page_size, self.kv_heads, self.head_dim, k.data_ptr(), v.data_ptr(),
                                   k_scales.data_ptr() if fmt == QARL_KV_E4M3 else None, v_scales.data_ptr() if fmt == QARL_KV_E4M3 else None)
         self.ref = C.byref(self.desc)
+        self.gpu = k.get_device()       # -1: host memory, which the calls refuse
 
     @staticmethod
     def empty(fmt, num_pages, page_size, kv_heads, head_dim, device="cuda"):
@@ -559,29 +575,29 @@ class KVCache:
         return KVCache(fmt, *[torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)])
 
 
-def _heads(t, name, shape):
+def _heads(t, name, shape, gpu):
     """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose heads are contiguous."""
     token, head, last = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.shape != shape or t.dtype is not _BF16 or not t.is_cuda or last != 1:
-        _wrong(t, name, "%s %s with contiguous heads" % (list(shape), _BF16))
+    if t.shape != shape or t.dtype is not _BF16 or t.get_device() != gpu or gpu < 0 or last != 1:
+        _wrong(t, name, "%s %s with contiguous heads" % (list(shape), _BF16), gpu)
     return t.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0      # (the stride of a single one may be anything)
 
 
-def _table(t, S):
+def _table(t, S, gpu):
     stride, last = t.stride() if t.dim() == 2 else (0, 0)
     width = t.shape[-1]
-    if t.shape != (S, width) or t.dtype is not _I32 or not t.is_cuda or (last != 1 and width > 1):
-        _wrong(t, "block_table", "[%d, pages] %s with contiguous rows" % (S, _I32))
+    if t.shape != (S, width) or t.dtype is not _I32 or t.get_device() != gpu or gpu < 0 or (last != 1 and width > 1):
+        _wrong(t, "block_table", "[%d, pages] %s with contiguous rows" % (S, _I32), gpu)
     return t.data_ptr(), stride if S > 1 else width, width
 
 
 def qarl_kv_cache_write(cache, k, v, slots):
     """Writes k, v [T, kv_heads, head_dim] (bf16, any token and head stride) into the slots [T] (int64) of the cache; see include/qarl.h."""
     T = slots.numel()
-    shape = (T, cache.kv_heads, cache.head_dim)
-    kp, kt, kh = _heads(k, "k", shape)
-    vp, vt, vh = _heads(v, "v", shape)
-    _check(lib().qarl_kv_cache_write(cache.ref, kp, kt, kh, vp, vt, vh, T, _flat(slots, "slots", _I64, (T,)), _raw_stream(k.get_device())))
+    shape, gpu = (T, cache.kv_heads, cache.head_dim), k.get_device()
+    kp, kt, kh = _heads(k, "k", shape, gpu)
+    vp, vt, vh = _heads(v, "v", shape, gpu)
+    _check(lib().qarl_kv_cache_write(_cache(cache, gpu), kp, kt, kh, vp, vt, vh, T, _flat(slots, "slots", _I64, (T,), gpu), _raw_stream(gpu)))
 
 
 def qarl_kv_cache_read(cache, block_table, offsets, total, out=None):
@@ -591,10 +607,10 @@ def qarl_kv_cache_read(cache, block_table, offsets, total, out=None):
     if out is None:
         out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=block_table.device) for _ in range(2))
     k, v = out
-    S = offsets.numel() - 1
-    tp, ts, tw = _table(block_table, S)
-    _check(lib().qarl_kv_cache_read(cache.ref, tp, ts, tw, _flat(offsets, "offsets", _I32, (S + 1,)), S, total, _flat(k, "k", _BF16, shape),
-                                    _flat(v, "v", _BF16, shape), _raw_stream(k.get_device())))
+    S, gpu = offsets.numel() - 1, block_table.get_device()
+    tp, ts, tw = _table(block_table, S, gpu)
+    _check(lib().qarl_kv_cache_read(_cache(cache, gpu), tp, ts, tw, _flat(offsets, "offsets", _I32, (S + 1,), gpu), S, total,
+                                    _flat(k, "k", _BF16, shape, gpu), _flat(v, "v", _BF16, shape, gpu), _raw_stream(gpu)))
     return k, v
 
 
@@ -609,22 +625,22 @@ def qarl_paged_attention(query, cache, block_table, kv_lens, q_offsets, max_q_le
     T, Hq, D = query.shape
     dev = query.device
     shape = (T, Hq, cache.head_dim)
-    S = kv_lens.numel()
+    S, gpu = kv_lens.numel(), query.get_device()
     if out is None:
         out = torch.empty(shape, dtype=torch.float32 if out_dtype == QARL_OUT_F32 else torch.bfloat16, device=dev)
     if lse is None and want_lse:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
-    qp, qt, qh = _heads(query, "query", shape)
-    tp, ts, tw = _table(block_table, S)
-    L, ref = lib(), cache.ref
+    qp, qt, qh = _heads(query, "query", shape, gpu)
+    tp, ts, tw = _table(block_table, S, gpu)
+    L, ref = lib(), _cache(cache, gpu)
     if ws is None:
         need = L.qarl_paged_attention_workspace_bytes(ref, T, Hq, S, max_q_len, max_kv_len)
         if need:
             ws = torch.empty((need,), dtype=_U8, device=dev)
-    wsp, wsn = _ws(ws)
+    wsp, wsn = _ws(ws, gpu)
     f32 = out.dtype is _F32
-    _check(L.qarl_paged_attention(qp, qt, qh, T, Hq, ref, tp, ts, tw, _flat(kv_lens, "kv_lens", _I32, (S,)), _flat(q_offsets, "q_offsets", _I32, (S + 1,)),
-                                  S, max_q_len, max_kv_len, D ** -0.5 if scale is None else scale, window, _flat(out, "out", _F32 if f32 else _BF16, shape),
-                                  QARL_OUT_F32 if f32 else QARL_OUT_BF16, None if lse is None else _flat(lse, "lse", _F32, (T, Hq)), wsp, wsn,
-                                  _raw_stream(query.get_device())))
+    _check(L.qarl_paged_attention(qp, qt, qh, T, Hq, ref, tp, ts, tw, _flat(kv_lens, "kv_lens", _I32, (S,), gpu), _flat(q_offsets, "q_offsets", _I32, (S + 1,), gpu),
+                                  S, max_q_len, max_kv_len, D ** -0.5 if scale is None else scale, window, _flat(out, "out", _F32 if f32 else _BF16, shape, gpu),
+                                  QARL_OUT_F32 if f32 else QARL_OUT_BF16, None if lse is None else _flat(lse, "lse", _F32, (T, Hq), gpu), wsp, wsn,
+                                  _raw_stream(gpu)))
     return dict(out=out, lse=lse)

@@ -151,3 +151,27 @@ def test_offsets_past_32_bits(q):
     q.qarl_kv_cache_write(small, k, v, slots - (pages - 1) * page)
     wk, wv = q.qarl_kv_cache_read(small, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([0, page], dtype=torch.int32, device="cuda"), page)
     assert torch.equal(rk, wk) and torch.equal(rv, wv) and rk[-3:].abs().sum() > 0
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_buffers_in_host_memory_are_refused(q, fmt):
+    """Beside operands on the GPU: a cache, a workspace or an index array in host memory reaches no kernel."""
+    host, c = q.KVCache.empty(_fmt(q, fmt), 4, 16, 2, 64, "cpu"), q.KVCache.empty(_fmt(q, fmt), 4, 16, 2, 64)
+    k = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    query = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    slots, table = torch.arange(2, device="cuda"), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    lens, offsets = torch.tensor([2], dtype=torch.int32, device="cuda"), torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    for call in (lambda a: q.qarl_kv_cache_write(a, k, k, slots), lambda a: q.qarl_kv_cache_read(a, table, offsets, 2),
+                 lambda a: q.qarl_paged_attention(query, a, table, lens, offsets, 2, 2)):
+        with pytest.raises(ValueError, match="cache must be on cuda"):
+            call(host)
+        call(c)
+    for bad in (torch.empty(4096, dtype=torch.uint8), torch.empty(8192, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="ws must be"):
+            q.qarl_paged_attention(query, c, table, lens, offsets, 2, 2, ws=bad)
+        with pytest.raises(ValueError, match="ws must be"):
+            q.qarl_add_rmsnorm_backward(k.view(2, 128), k.view(2, 128), k.view(-1)[:128], 1e-6, ws=bad)
+    with pytest.raises(ValueError, match="slots must be"):
+        q.qarl_kv_cache_write(c, k, k, slots.cpu())
+    with pytest.raises(ValueError, match="block_table must be"):
+        q.qarl_paged_attention(query, c, table.cpu(), lens, offsets, 2, 2)

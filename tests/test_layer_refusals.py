@@ -180,3 +180,25 @@ def test_reference_attention_on_closed_forms():
     assert torch.equal(out[:, 0], v[2:, 0]) and (lse == 0).all()
     out, lse, _, _ = ref.attention(q, k, v, torch.ones(5, dtype=torch.bool), 1, 1.0, 0)       # two queries in front of the first position
     assert (out[:2] == 0).all() and (lse[:2] == -float("inf")).all() and torch.equal(out[2, 0], v[0, 0])
+
+
+def test_binding_refuses_buffers_that_a_kernel_cannot_reach(q):
+    """Host memory, another GPU, strided workspaces: every pointer of a call is looked at, the cache's and the workspace's too."""
+    c = q.KVCache.empty(q.QARL_KV_E4M3, 4, 16, 2, 64, "cpu")
+    for gpu in (0, 3, -1):
+        with pytest.raises(ValueError, match="cache must be on"):
+            q._cache(c, gpu)
+        with pytest.raises(ValueError, match="ws must be"):
+            q._ws(torch.empty(64, dtype=torch.uint8), gpu)
+        with pytest.raises(ValueError, match="y must be"):
+            q._rows(torch.zeros((4, 64), dtype=torch.bfloat16), "y", torch.bfloat16, (4, 64), gpu)
+        with pytest.raises(ValueError, match="lse must be"):
+            q._flat(torch.zeros((4, 8)), "lse", torch.float32, (4, 8), gpu)
+        with pytest.raises(ValueError, match="v must be"):
+            q._heads(torch.zeros((4, 2, 64), dtype=torch.bfloat16), "v", (4, 2, 64), gpu)
+        with pytest.raises(ValueError, match="block_table must be"):
+            q._table(torch.zeros((4, 2), dtype=torch.int32), 4, gpu)
+    assert q._ws(None, 0) == (None, 0)
+    for bad in (dict(v=c.v.to("meta")), dict(k_scales=c.k_scales.to("meta")), dict(v_scales=c.v_scales.to("meta"))):
+        with pytest.raises(ValueError, match="one device"):
+            q.KVCache(q.QARL_KV_E4M3, **dict(dict(k=c.k, v=c.v, k_scales=c.k_scales, v_scales=c.v_scales), **bad))
