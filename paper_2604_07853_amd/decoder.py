@@ -3,7 +3,7 @@
     residual add + RMS norm -> q, k, v projection -> paged cache (written quantized or plain) -> attention over it -> o projection
     -> residual add + RMS norm (its output also as the experts' e4m3 rows) -> router -> quantized experts
 
-The projections are the grouped GEMM with one expert.  Positions are the caller's: `rotate(q, k)`, called on the views of the
+The projections are the grouped GEMM with one expert, on bf16 rows: W4A16 weights.  Positions are the caller's: `rotate(q, k)`, called on the views of the
 new tokens' queries and keys before they are cached, applies what the model uses.  The router's logits are a plain library product.
 """
 import torch
@@ -12,8 +12,8 @@ from . import binding as q
 
 
 class DecoderLayer:
-    """norm1, norm2 bf16 [H]; qkv QWeight [1, (heads + 2 kv_heads) * head_dim, H]; o QWeight [1, H, heads * head_dim]; router bf16 [experts, H];
-    gate_up, down the experts' QWeights; cache a KVCache of this layer."""
+    """norm1, norm2 bf16 [H]; qkv QWeight [1, (heads + 2 kv_heads) * head_dim, H]; o QWeight [1, H, heads * head_dim], both W4A16; router bf16
+    [experts, H]; gate_up, down the experts' QWeights, of any format; cache a KVCache of this layer."""
 
     def __init__(self, norm1, qkv, o, norm2, router, gate_up, down, cache, topk=8, eps=1e-6):
         D = cache.head_dim
@@ -21,8 +21,18 @@ class DecoderLayer:
         if (qkv.E, qkv.N, qkv.K) != (1, (self.heads + 2 * cache.kv_heads) * D, self.H) or o.E != 1 or o.K != self.heads * D:
             raise ValueError("qkv and o must be one matrix each, [(heads + 2 kv_heads) * head_dim, H] and [H, heads * head_dim] (got %s, %s)"
                              % ((qkv.E, qkv.N, qkv.K), (o.E, o.N, o.K)))
+        if qkv.fmt in q.E4M3_ACT_FORMATS or o.fmt in q.E4M3_ACT_FORMATS:
+            raise ValueError("qkv and o run on bf16 rows: QARL_W4A16_G128 weights (got formats %d, %d)" % (qkv.fmt, o.fmt))
+        if self.heads % cache.kv_heads:
+            raise ValueError("%d query heads on %d cached ones" % (self.heads, cache.kv_heads))
         if norm1.shape != (self.H,) or norm2.shape != (self.H,) or router.shape != (gate_up.E, self.H) or gate_up.K != self.H:
             raise ValueError("norms must be [%d], router [%d, %d] and gate_up of K = %d" % (self.H, gate_up.E, self.H, self.H))
+        # the experts' kernels write down's rows and columns into the layer's own buffers
+        if (down.E, down.N, 2 * down.K) != (gate_up.E, self.H, gate_up.N) or (gate_up.fmt in q.E4M3_ACT_FORMATS) != (down.fmt in q.E4M3_ACT_FORMATS):
+            raise ValueError("down must be [%d, %d, %d] on rows of gate_up's kind (got %s, formats %d and %d)"
+                             % (gate_up.E, self.H, gate_up.N // 2, (down.E, down.N, down.K), gate_up.fmt, down.fmt))
+        if gate_up.E % 64 or gate_up.E > 256 or not 1 <= topk <= min(gate_up.E, 32):
+            raise ValueError("the router takes 64, 128, 192 or 256 experts and picks 1 to 32 (got %d, %d)" % (gate_up.E, topk))
         self.norm1, self.qkv, self.o, self.norm2, self.router = norm1, qkv, o, norm2, router
         self.gu, self.dn, self.cache, self.topk, self.eps = gate_up, down, cache, topk, eps
         self.e4m3_rows = gate_up.fmt in q.E4M3_ACT_FORMATS

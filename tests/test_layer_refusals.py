@@ -202,3 +202,30 @@ def test_binding_refuses_buffers_that_a_kernel_cannot_reach(q):
     for bad in (dict(v=c.v.to("meta")), dict(k_scales=c.k_scales.to("meta")), dict(v_scales=c.v_scales.to("meta"))):
         with pytest.raises(ValueError, match="one device"):
             q.KVCache(q.QARL_KV_E4M3, **dict(dict(k=c.k, v=c.v, k_scales=c.k_scales, v_scales=c.v_scales), **bad))
+
+
+def test_decoder_layer_refuses_what_it_cannot_run(q):
+    """In the constructor, and not in the middle of the first step: e4m3 projections, head counts that do not divide, experts whose down does not fit."""
+    from paper_2604_07853_amd.decoder import DecoderLayer
+    H, heads, kv, D, E, I = 256, 4, 2, 64, 64, 128
+    weight = lambda fmt, e, n, k: q.QWeight.empty(fmt, e, n, k, "cpu")
+    norm = torch.ones(H, dtype=torch.bfloat16)
+    good = dict(norm1=norm, norm2=norm, qkv=weight(q.QARL_W4A16_G128, 1, (heads + 2 * kv) * D, H), o=weight(q.QARL_W4A16_G128, 1, H, heads * D),
+                router=torch.zeros((E, H), dtype=torch.bfloat16), gate_up=weight(q.QARL_FP8_E4M3_CH, E, 2 * I, H), down=weight(q.QARL_FP8_E4M3_CH, E, H, I),
+                cache=q.KVCache.empty(q.QARL_KV_BF16, 4, 16, kv, D, "cpu"), topk=8)
+    DecoderLayer(**good)
+    DecoderLayer(**dict(good, gate_up=weight(q.QARL_W4A8_G128, E, 2 * I, H)))          # both on e4m3 rows
+    for fmt in q.E4M3_ACT_FORMATS:
+        with pytest.raises(ValueError, match="bf16 rows"):
+            DecoderLayer(**dict(good, qkv=weight(fmt, 1, (heads + 2 * kv) * D, H)))
+        with pytest.raises(ValueError, match="bf16 rows"):
+            DecoderLayer(**dict(good, o=weight(fmt, 1, H, heads * D)))
+    with pytest.raises(ValueError, match="query heads"):
+        DecoderLayer(**dict(good, cache=q.KVCache.empty(q.QARL_KV_BF16, 4, 16, 3, D, "cpu"), qkv=weight(q.QARL_W4A16_G128, 1, (heads + 6) * D, H)))
+    for down in (weight(q.QARL_FP8_E4M3_CH, E, H, 2 * I), weight(q.QARL_FP8_E4M3_CH, E, 2 * H, I), weight(q.QARL_FP8_E4M3_CH, 2 * E, H, I),
+                 weight(q.QARL_W4A16_G128, E, H, I)):
+        with pytest.raises(ValueError, match="down must be"):
+            DecoderLayer(**dict(good, down=down))
+    for topk in (0, 33):
+        with pytest.raises(ValueError, match="picks 1 to 32"):
+            DecoderLayer(**dict(good, topk=topk))
