@@ -38,6 +38,8 @@ class DecoderLayer:
         self.e4m3_rows = gate_up.fmt in q.E4M3_ACT_FORMATS
         self._moe = {}          # decode batches, up to 512 tokens: the experts' layer object by number of tokens,
         self._room = None       # all on the buffers of the largest (a server meets every number of them, and a captured step keeps its addresses)
+        self._stream = None     # the stream that last used those buffers, and its handle
+        self._handle = None
         self._one = {}          # and the row offsets of a projection, [0, T]
 
     def _project(self, W, x):
@@ -49,9 +51,21 @@ class DecoderLayer:
                 self._one[T] = offsets
         return q.qarl_qgemm_grouped(W, x, offsets, T)
 
+    def _take_buffers(self, y):
+        """The buffers of batches of up to 512 belong to one call at a time: a call on another stream waits for what the last one's stream holds."""
+        handle = torch._C._cuda_getCurrentRawStream(y.get_device())
+        if handle == self._handle or torch.cuda.is_current_stream_capturing():      # (a graph's replays are ordered by whoever replays it)
+            return
+        stream = torch.cuda.current_stream(y.device)
+        if self._stream is not None:
+            stream.wait_stream(self._stream)
+        self._stream, self._handle = stream, handle
+
     def _experts(self, y, codes, scales):
         T = y.shape[0]
         logits = torch.matmul(y, self.router.t())
+        if T <= 512:
+            self._take_buffers(y)
         if codes is None:
             moe = self._moe.get(T)
             if moe is None:     # few tokens: one call, the experts' kernels read (and quantize) the bf16 rows themselves
@@ -75,7 +89,8 @@ class DecoderLayer:
         """x [T, H] bf16: what the layer before has computed; residual [T, H]: the residual stream so far (None in front of the first layer).  slots,
         block_table, kv_lens, q_offsets, max_q_len, max_kv_len: as for qarl_kv_cache_write and qarl_paged_attention, kv_lens with the new tokens.
         Returns (output, residual) for the next layer, whose first norm adds them.  Up to 512 tokens the output is the layer's own buffer, written
-        again by its next call of up to 512."""
+        again by its next call of up to 512, on whatever stream: such calls wait for the stream of the call before (and for its reader there); the replays
+        of a captured step and other calls are for the caller to order."""
         T, c = x.shape[0], self.cache
         n1 = q.qarl_add_rmsnorm(x, self.norm1, self.eps, residual=residual)
         residual = x if residual is None else n1["residual"]

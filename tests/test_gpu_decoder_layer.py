@@ -120,3 +120,25 @@ def test_batches_of_every_size_share_one_set_of_buffers(q, fmt):
     assert len(layer._moe) == 5
     for name in ("a", "out"):
         assert len({getattr(m, name).untyped_storage().data_ptr() for m in layer._moe.values()}) == 1
+
+
+@pytest.mark.parametrize("fmt", ["QARL_W4A16_G128", "QARL_FP8_E4M3_CH"])
+def test_batches_on_two_streams(q, fmt):
+    """Chunks on one stream and decode steps on another, each result read late: it is that of the same call alone."""
+    calls, per = [(300, 0), (7, 1), (512, 0), (1, 1), (300, 1), (7, 0)], 32
+    inputs = []
+    for i, (T, _) in enumerate(calls):      # sequences of their own, in pages of their own
+        p = plan([T], [0], per)
+        inputs.append((synth.normal_bf16((T, H), 1.0, 60 + i).cuda(), dict(p, slots=p["slots"] + i * per * PAGE, block_table=p["block_table"] + i * per)))
+    make = lambda: layer_of(q, getattr(q, fmt), q.QARL_KV_BF16, per * len(calls))
+    want = [make().forward(x, None, **p)[0].clone() for x, p in inputs]
+    layer, streams, got = make(), [torch.cuda.Stream(), torch.cuda.Stream()], []
+    torch.cuda.synchronize()
+    for (x, p), (_, on) in zip(inputs, calls):
+        with torch.cuda.stream(streams[on]):
+            out = layer.forward(x, None, **p)[0]
+            torch.cuda._sleep(5_000_000)
+            got.append(out.clone())
+    torch.cuda.synchronize()
+    for (T, _), a, b in zip(calls, got, want):
+        assert torch.equal(a, b), T
