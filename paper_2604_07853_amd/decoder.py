@@ -46,8 +46,8 @@ class DecoderLayer:
         T = x.shape[0]
         offsets = self._one.get(T)
         if offsets is None:
-            offsets = torch.tensor([0, T], dtype=torch.int32, device=x.device)
-            if T <= 512:
+            offsets = torch.arange(2, dtype=torch.int32, device=x.device).mul_(T)       # made on the GPU: a graph capture takes no copy from the host
+            if T <= 512 and not torch.cuda.is_current_stream_capturing():               # (and fills what it makes when it is replayed)
                 self._one[T] = offsets
         return q.qarl_qgemm_grouped(W, x, offsets, T)
 

@@ -142,3 +142,38 @@ def test_batches_on_two_streams(q, fmt):
     torch.cuda.synchronize()
     for (T, _), a, b in zip(calls, got, want):
         assert torch.equal(a, b), T
+
+
+@pytest.mark.parametrize("fmt,kv_fmt", [("QARL_W4A16_G128", "QARL_KV_BF16"), ("QARL_FP8_E4M3_CH", "QARL_KV_E4M3"), ("QARL_W4A8_G128", "QARL_KV_BF16")])
+@pytest.mark.parametrize("T", [7, 600])
+@pytest.mark.parametrize("met", [True, False])
+def test_captured_steps(q, fmt, kv_fmt, T, met):
+    """A step in a graph, of a size met before and of a new one: every replay gives what the same call gives outside, before and after it."""
+    pages = 64
+    layer = layer_of(q, getattr(q, fmt), getattr(q, kv_fmt), pages)
+    x, r = (synth.normal_bf16((T, H), 1.0, s).cuda() for s in (70, 71))
+    p = plan([T], [20], pages)
+    for t in (layer.cache.k, layer.cache.v, layer.cache.k_scales, layer.cache.v_scales):
+        if t is not None:
+            t.zero_()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for n in (5, 700) + ((T,) if met else ()):
+            layer.forward(synth.normal_bf16((n, H), 1.0, n).cuda(), None, **plan([n], [0], pages))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, stream = layer.forward(x, r, **p)
+    if not met:         # a call of that size outside, in front of the first replay
+        first = [t.clone() for t in layer.forward(x, r, **p)]
+    for seed in range(3):
+        if seed:
+            x.copy_(synth.normal_bf16((T, H), 1.0, 80 + seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), stream.clone()
+        if seed == 0 and not met:
+            assert all(torch.equal(a, b) for a, b in zip(first, got))
+        want = layer.forward(x, r, **p)
+        torch.cuda.synchronize()
+        assert got[0].isfinite().all() and all(torch.equal(a, b) for a, b in zip(got, want)), seed
