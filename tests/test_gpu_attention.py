@@ -403,3 +403,28 @@ def test_scales_below_the_smallest_normal_ones(q, fmt, n, scale):
         tol = mag[0] * (ref.HALF_BF16 + 2 * err[:, None] + 2.0 ** -19) + o[0].abs() * 1.01 * ref.HALF_BF16
         assert ((got["out"][i].double().cpu() - o[0]).abs() <= tol).all(), (i, float(top.max()))
         assert ((got["lse"][i].double().cpu() - e[0]).abs() <= err + 2.0 ** -19 * (1 + e[0].abs())).all(), (i, float(top.max()))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(65, 1, 64), (96, 1, 128), (160, 2, 64), (256, 1, 64)])
+def test_more_query_heads_per_cached_one_than_few_rows_hold(q, fmt, heads, kv_heads, dim):
+    """Single tokens whose heads alone are more than the kernel for few rows takes, and up to a whole row block per token."""
+    seqs = [(1, 1), (1, 700), (3, 65), (0, 9), (1, 0), (2, 1300)]
+    m = make(q, fmt, seqs, heads, kv_heads, dim, 16, heads)
+    check(m, call(q, m))
+    m = make(q, fmt, [(1, 3000), (1, 40)], heads, kv_heads, dim, 16, heads + 1)
+    check(m, call(q, m, window=700), window=700)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("max_q,max_kv", [(1, 20000), (2, 700), (64, 20000), (2048, 1 << 20), (1 << 30, 1 << 24)])
+def test_bounds_that_no_sequence_reaches(q, fmt, max_q, max_kv):
+    """max_q_len and max_kv_len as a server names them, once and for all: the results stay within the same bound."""
+    seqs = [(1, 600), (1, 33), (1, 0), (1, 1)] if max_q == 1 else [(1, 600), (2, 33), (0, 4), (2, 130)]
+    m = make(q, fmt, seqs, 16, 2, 64, 16, 61)
+    got = q.qarl_paged_attention(m["query"].cuda()[:, 1:17], m["c"], m["table"].cuda(), m["kv_lens"].cuda(), m["offsets"].cuda(), max_q, max_kv, want_lse=True)
+    check(m, got)
+    many = make(q, fmt, [(70, 300), (1, 900), (5, 5)], 16, 2, 64, 16, 62)
+    if max_q > 70:
+        check(many, q.qarl_paged_attention(many["query"].cuda()[:, 1:17], many["c"], many["table"].cuda(), many["kv_lens"].cuda(), many["offsets"].cuda(), max_q,
+                                           max_kv, window=100, want_lse=True), window=100)

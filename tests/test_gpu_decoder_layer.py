@@ -177,3 +177,19 @@ def test_captured_steps(q, fmt, kv_fmt, T, met):
         want = layer.forward(x, r, **p)
         torch.cuda.synchronize()
         assert got[0].isfinite().all() and all(torch.equal(a, b) for a, b in zip(got, want)), seed
+
+
+@pytest.mark.parametrize("fmt", ["QARL_W4A16_G128", "QARL_FP8_E4M3_CH"])
+def test_no_tokens(q, fmt):
+    """A step without tokens, alone and between others."""
+    layer = layer_of(q, getattr(q, fmt), q.QARL_KV_BF16, 8)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none = dict(slots=torch.empty(0, dtype=torch.int64, device="cuda"), block_table=torch.zeros((3, 2), **i32), kv_lens=torch.zeros(3, **i32),
+                q_offsets=torch.zeros(4, **i32), max_q_len=1, max_kv_len=1)
+    x = synth.normal_bf16((3, H), 1.0, 5).cuda()
+    for _ in range(2):
+        for stream in (None, x[:0]):
+            out, res = layer.forward(x[:0], stream, **none)
+            assert out.shape == res.shape == (0, H)
+        want = [t.clone() for t in layer.forward(x, None, **plan([3], [0], 8))]
+        assert want[0].isfinite().all()
