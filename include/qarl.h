@@ -304,7 +304,7 @@ int qarl_tbpo_objective(const float *lp_current, const float *lp_old, const floa
  *       and that qarl_qgemm_routed makes of it inside, so that both engines run on the same codes.  A zero row gets scale 0 and
  *       codes 0; a row with a NaN or an infinity among its y gets scale NaN and NaN codes.
  * stream_dtype (QARL_OUT_BF16 or QARL_OUT_F32) is the type of residual and residual_out.  Strides are the elements between rows.
- * residual_out may be residual or x itself, y_bf16 may be x (same pointer and stride); outputs may not overlap inputs otherwise.
+ * residual_out may be residual or, where the stream is bf16, x itself, y_bf16 may be x (same pointer and stride); outputs may not overlap inputs otherwise.
  * Supported: K % 8 == 0, K <= 16384, strides multiples of 8, buffers 16-byte (codes: 8-byte) aligned, eps >= 0 and finite.
  * rows == 0 is a no-op. */
 int qarl_add_rmsnorm(const void *x_bf16, int64_t x_stride, const void *residual, int64_t residual_stride,

@@ -1,8 +1,8 @@
 // Attention of few query rows per sequence (single tokens, a few speculated ones) over the paged cache.
 // Bound by memory: G query heads share a cached one, 4 G D operations per 4 D bytes.  A workgroup takes one (sequence, cached head, piece
 // of the cache); its four wavefronts take every fourth tile of 32 positions each, with running maxima and sums of their own, which they
-// join at the end.  (32 query heads on 4 of 128, 256 sequences of 4096 positions: bf16 362 us, 5.9 TB/s, e4m3 197 us, 5.6; 256 of up to 18432 e4m3 455 us, 5.3; one of 18432, where
-// lengths, pages and keys wait for one another, 10.7 us.)  Keys and values flow through rings in LDS, private to a wavefront and filled by asynchronous copies, so that a wavefront waits
+// join at the end.  (32 query heads on 4 of 128, 256 sequences of 4096 positions: bf16 361 us, 6.0 TB/s, e4m3 196 us, 5.7; 256 of up to 18432 e4m3 453 us, 5.3; one of 18432, where
+// lengths, pages and keys wait for one another, 10.6 us.)  Keys and values flow through rings in LDS, private to a wavefront and filled by asynchronous copies, so that a wavefront waits
 // for its own copies only and no barrier stands in the loop.
 //
 // S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions: lane (n = lane & 15, q = lane >> 4) then holds the scores of row n at

@@ -90,7 +90,9 @@ inline int64_t few_pieces(int64_t units, int64_t len, int64_t extra)
 //   From 256 (sequence, head)s on about four pieces per CU at the longest length, for the lengths are not known here: 64 ragged sequences of up to
 //   18000, 4 heads, 8 / 32 / 64 rows with one piece 232 / 253 / 327, with four 211 / 232 / 290 (of equal lengths 8000, 32 / 64 rows, the other way:
 //   190 / 204 against 207 / 244).  Below that few_pieces(): 16 of 4096, 8 / 64 rows 34 / 46 instead of 40 / 69 with four pieces per CU; 48 of 12000, 64 rows,
-//   with 256 / 512 / 768 / 1024 wanted 282 / 300 / 257 / 282.
+//   with 256 / 512 / 768 / 1024 wanted 282 / 300 / 257 / 282 (24 ragged ones of up to 12000, 64 rows, lose: 114 instead of 109).
+//   At the border one and four pieces are close, 252 and 256 (sequence, head)s alike: 64 sequences of up to 9000 with one / four, single tokens bf16 211 / 212, e4m3
+//   117 / 121, ragged 118 / 115 and 81 / 65; 64 rows 238 / 264, 186 / 208, ragged 167 / 164, 151 / 146; 63 sequences within 3 % of that, e4m3 ragged 82 / 65.
 //   Many rows: a workgroup per CU; beyond 128 blocks a cut costs what it fills (1 x 2048 over 16384, 256 blocks: 626 us whole, 658 in two; 512 over 8192, 64
 //   blocks: 244 whole, 92 in four, 107 in eight; 4 x 300 over 4000, 160 blocks: 133 whole, 158 in two, 151 in four; 2 x 700 over 12000, 176 blocks: 419
 //   whole, 450 in two, 393 in four).

@@ -11,9 +11,10 @@
 // A wavefront's own work overlaps: step s (32 positions) computes the scores of step s + 1 and adds the values of step s - 1 on the matrix cores while the
 // vector units turn the scores of step s into probabilities; none of the three waits for another.
 //
-// Measured, 32 query heads on 4 cached ones of 128: eight prompts of 2048 bf16 347 us (275 GFLOP, 792 TFLOP/s), 4 x 2048 over 16384 cached positions
-// 2266 us (1031 TFLOP/s); 28 heads on 4, 12 chunks of mixed lengths over an e4m3 cache 335 us (776 TFLOP/s).  A tile takes 4040-4160 cycles, 2048 of
-// them products; a block 7 us more to start and end.
+// Measured, 32 query heads on 4 cached ones of 128, calls on end: eight prompts of 2048 bf16 352 us (275 GFLOP, 781 TFLOP/s), e4m3 384 (716), with a window of
+// 512 210 (572), head_dim 64 236 (584); 4 x 2048 over 16384 cached positions 2288 us (1021 TFLOP/s); 28 heads on 4, 12 chunks of mixed lengths over an e4m3
+// cache 332 us (781 TFLOP/s).  The first ten calls after a pause of 50 ms take 438 us for the prompts and 419 for the chunks; under the profiler 384 and 345.  A
+// tile takes 4040-4160 cycles, 2048 of them products; a block 7 us more to start and end.
 #include "attention.hpp"
 
 namespace qarl {
