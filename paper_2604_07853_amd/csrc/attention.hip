@@ -1,4 +1,4 @@
-// Attention over the paged cache: how a call is split between the kernels and along the cache, and the join of the pieces.
+// Attention over the paged cache: the workspace, the launches and the join of the pieces (how a call is split: attention_split.hpp).
 #include "attention.hpp"
 
 namespace qarl {
