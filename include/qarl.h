@@ -291,7 +291,7 @@ int qarl_tbpo_objective(const float *lp_current, const float *lp_old, const floa
 
 /* ---- The other half of a decoder layer: residual addition with RMS norm, the paged KV cache, attention over it.
  * Section 3.1's two engines run it around the quantized experts; the paper gives no kernel for it.  Positions are the
- * caller's: q and k arrive with whatever rotation the model applies. */
+ * caller's: q and k arrive with whatever rotation the model applies (qarl_rotary), or are turned on their way into the cache (qarl_rotary_kv_write). */
 
 /* h = x + residual in fp32 (x alone where residual is NULL), then per row of K
  *   y = h * rstd * weight,  rstd = 1 / sqrt(mean_k h^2 + eps),
@@ -330,13 +330,17 @@ int qarl_add_rmsnorm_backward(const void *dy_bf16, int64_t dy_stride, const void
  *   KV_BF16: k, v bf16  [num_pages][kv_heads][page_size][head_dim]
  *   KV_E4M3: k, v uint8 of the same shape (e4m3 bit patterns), k_scales, v_scales float [num_pages][kv_heads][page_size]: the FP
  *            quantizer of section 2.2 with one scale per token and head; value = scale * code.
+ *   KV_E2M1: k, v uint8 [num_pages][kv_heads][page_size][head_dim / 2], two e2m1 codes a byte, the even element in the low bits (codes as for
+ *            FP4_E2M1_CH), k_scales, v_scales uint8 [num_pages][kv_heads][page_size][4]: each quarter of a row (head_dim / 4 neighbouring elements) has
+ *            a power of two for its scale, 2^(byte - 127), byte 255: NaN; value = scale * code.  The quantizer takes the smallest scale from 2^-100
+ *            to 2^125 with 6 * scale >= absmax of the quarter and code = e2m1_rne_saturating(x / scale); a zero quarter gets 2^-100 and codes 0.
  * Requirements: head_dim 64 or 128, page_size a power of two from 8 to 1024, kv_heads <= 1024, buffers 16-byte aligned. */
-typedef enum { QARL_KV_BF16 = 1, QARL_KV_E4M3 = 2 } qarl_kv_format;
+typedef enum { QARL_KV_BF16 = 1, QARL_KV_E4M3 = 2, QARL_KV_E2M1 = 3 } qarl_kv_format;
 typedef struct {
     int32_t fmt; /* qarl_kv_format */
     int32_t num_pages, page_size, kv_heads, head_dim;
     void *k, *v;
-    float *k_scales, *v_scales; /* KV_E4M3 only */
+    void *k_scales, *v_scales; /* KV_E4M3: float, KV_E2M1: uint8 */
 } qarl_kv_cache;
 
 /* Bytes of k (and of v), of k_scales (and of v_scales); 0 for an unknown format or non-positive sizes. */
@@ -345,7 +349,8 @@ size_t qarl_kv_scales_bytes(int fmt, int num_pages, int page_size, int kv_heads,
 
 /* Writes T tokens into the cache: token t, head h comes from k_bf16 + t * k_token_stride + h * k_head_stride (elements; head_dim
  * contiguous; v likewise) and goes to slot slots[t]; KV_E4M3 quantizes it on the way (scale = absmax / 448, code = e4m3_rne(x / scale),
- * IEEE divides; zero rows: scale 0, codes 0; rows with a NaN or an infinity: scale NaN, NaN codes).  A slot outside
+ * IEEE divides; zero rows: scale 0, codes 0; rows with a NaN or an infinity: scale NaN, NaN codes), KV_E2M1 as above (quarters with a NaN or an infinity:
+ * scale byte 255, codes 0).  A slot outside
  * [0, num_pages * page_size) is skipped.  Of two tokens with the same slot one or a mixture is kept.
  * Strides multiples of 8, k and v 16-byte aligned.  T == 0 is a no-op. */
 int qarl_kv_cache_write(const qarl_kv_cache *cache, const void *k_bf16, int64_t k_token_stride, int64_t k_head_stride,
@@ -357,6 +362,49 @@ int qarl_kv_cache_write(const qarl_kv_cache *cache, const void *k_bf16, int64_t 
  * past the table and pages outside [0, num_pages) read as zeros.  total == 0 is a no-op. */
 int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, int64_t table_stride, int table_width,
                        const int32_t *offsets, int S, int64_t total, void *k_out_bf16, void *v_out_bf16, void *stream);
+
+/* Rotary positions.  Pair i of a head (i < rotary_dim / 2) is turned by the angle p * f_i at position p and multiplied by `amplitude`:
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ *   ROPE_HALF:  a = x[i], b = x[rotary_dim / 2 + i];     ROPE_PAIRS:  a = x[2 i], b = x[2 i + 1]
+ * Elements from rotary_dim on are passed on as they are.  The descriptor is host memory, made once and read during the call: it holds f_i / 2 pi as a 64-bit
+ * fraction of a turn, so that angles are exact modulo a turn at every position (fp32 products p * f_i are not).
+ *   qarl_rope_frequencies: f_i = base^(-2 i / rotary_dim), scaled for contexts longer than the model was trained on:
+ *     PLAIN   as they are
+ *     LINEAR  f_i / factor (positions interpolated)
+ *     YARN    f_i for pairs that make more than `high` turns within original_len, f_i / factor for those of less than `low`, in between linearly by the
+ *             number of the pair (from the pair, rounded down, that makes `high` turns to that, rounded up, of `low`); amplitude 0.1 ln factor + 1
+ *     BANDS   the same ends, in between linearly by the turns themselves; amplitude 1
+ *   qarl_rope_init: the descriptor, from these or from any other frequencies in [0, pi) radians a position.
+ * Supported: rotary_dim % 16 == 0, rotary_dim <= 2 * QARL_ROPE_MAX_PAIRS. */
+enum { QARL_ROPE_MAX_PAIRS = 128 };
+typedef enum { QARL_ROPE_HALF = 0, QARL_ROPE_PAIRS = 1 } qarl_rope_layout;
+typedef enum { QARL_ROPE_PLAIN = 0, QARL_ROPE_LINEAR = 1, QARL_ROPE_YARN = 2, QARL_ROPE_BANDS = 3 } qarl_rope_scaling;
+typedef struct {
+    int32_t rotary_dim, layout;
+    float amplitude;
+    uint64_t turns[QARL_ROPE_MAX_PAIRS];
+} qarl_rope;
+int qarl_rope_frequencies(int rotary_dim, double base, int scaling, double factor, double original_len, double low, double high,
+                          double *inv_freq, float *amplitude);
+int qarl_rope_init(qarl_rope *rope, int rotary_dim, int layout, const double *inv_freq, float amplitude);
+
+/* Turns the heads of T tokens at positions[t] (int64, any value): q [T][q_heads][head_dim] and k [T][k_heads][head_dim] (either may have 0 heads) of dtype
+ * (QARL_OUT_BF16 or QARL_OUT_F32) at their token and head strides (elements; head_dim contiguous) into q_out and k_out, rounded once from fp32.
+ * inverse != 0 turns the other way, amplitude included: the gradient of q and k, from that of their outputs.  An output may be its input (same pointer and
+ * strides); otherwise outputs may not overlap inputs or each other.
+ * Supported: head_dim % 16 == 0, rotary_dim <= head_dim <= 1024, strides of whole 16 bytes, pointers 16-byte aligned.  T == 0 is a no-op. */
+int qarl_rotary(const qarl_rope *rope, const int64_t *positions, int64_t T, int head_dim, int dtype, const void *q, int64_t q_token_stride,
+                int64_t q_head_stride, int q_heads, void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, const void *k,
+                int64_t k_token_stride, int64_t k_head_stride, int k_heads, void *k_out, int64_t k_out_token_stride, int64_t k_out_head_stride,
+                int inverse, void *stream);
+
+/* qarl_rotary on q (q_heads may be 0) and qarl_kv_cache_write of k, turned the same way, and v, in one launch, every format of the cache.  The turned keys are
+ * rounded once: the quantized formats quantize the fp32 values.  Slots outside the cache are skipped (their q is turned all the same).  Strides and
+ * alignments as for those two calls; q_out may be q. */
+int qarl_rotary_kv_write(const qarl_kv_cache *cache, const qarl_rope *rope, const int64_t *positions, int64_t T, const void *q_bf16, int64_t q_token_stride,
+                         int64_t q_head_stride, int q_heads, void *q_out_bf16, int64_t q_out_token_stride, int64_t q_out_head_stride, const void *k_bf16,
+                         int64_t k_token_stride, int64_t k_head_stride, const void *v_bf16, int64_t v_token_stride, int64_t v_head_stride,
+                         const int64_t *slots, void *stream);
 
 /* Causal attention of new tokens over the cache, which holds their keys and values already.  Sequence s has the query rows
  * [q_offsets[s], q_offsets[s+1]) (n of them: one when it is decoded, a chunk or all of a prompt when it is filled in) and kv_lens[s]
@@ -372,6 +420,7 @@ int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, i
  *   [0, num_pages) hold nothing: their positions are not seen.
  *   ws: qarl_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (0 for calls that are not split along the cache); what it
  *   holds before the call does not matter.
+ * KV_E2M1: codes times scales are exact in bf16, so that the attention is that over a bf16 cache of the same values.
  * A sequence's cache is split where there are few rows; a row's result depends on its sequence and on (T, S, the heads, max_q_len,
  * max_kv_len, window), not on timing.  Supported: q_heads % kv_heads == 0, q_heads <= 1024, T * (q_heads / kv_heads) <= 2^31 - 2^16.
  * max_kv_len <= 2^28, |scale| <= 1e38.  T == 0 or S == 0 is a no-op. */
@@ -382,6 +431,25 @@ int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_h
                          const int32_t *kv_lens, const int32_t *q_offsets, int S, int max_q_len, int max_kv_len,
                          float scale, int window, void *out, int out_dtype, float *lse, void *ws, size_t ws_bytes,
                          void *stream);
+
+/* The next token of each of T rows of V logits z (bf16 or fp32, rows at row_stride elements) from one given random number u[t] a row, usually uniform
+ * in [0, 1).  Tokens stand in the order of (logit descending, index ascending) and weigh w_i = exp((z_i - max z) / temperature[t]).  Kept is a beginning of that
+ * order, the shortest that one of these leaves, but one token at least:
+ *   top_k[t] > 0       its first top_k tokens
+ *   top_p[t] < 1       of those the shortest beginning that holds at least top_p of their weight
+ *   min_p[t] > 0       tokens with w_i >= min_p (relative to the most likely one)
+ * token[t] is the first kept token at which the running sum of the weights exceeds u * (weight of the kept) (the last kept one for u >= 1, the first for u < 0
+ * or NaN).  temperature[t] == 0: the first token, log-probs those of temperature 1.
+ *   logprob[t]       ln of the token's share of all V: the sampler's log-prob that qarl_logprob_mismatch compares (may be NULL)
+ *   kept_logprob[t]  ln of its share of what is kept (may be NULL)
+ * temperature, top_k, top_p and min_p may each be NULL (1, and no truncation).  A row with a NaN or +inf, without a finite logit, or with a temperature
+ * that is negative, infinite or NaN gets token -1 and NaN.  A logit of -inf is never chosen.
+ * Weights are computed in 64 bits and summed in 64-bit integers in units of 2^-43 of the largest: a row's result does not depend on timing or on the other rows.
+ * ws: qarl_sample_workspace_bytes(T, V) bytes, 16-byte aligned; what it holds before the call does not matter.
+ * Supported: V <= 2^20.  T == 0 is a no-op. */
+size_t qarl_sample_workspace_bytes(int T, int V);
+int qarl_sample(const void *logits, int dtype, int64_t row_stride, int T, int V, const float *u, const float *temperature, const int32_t *top_k,
+                const float *top_p, const float *min_p, int32_t *token, float *logprob, float *kept_logprob, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

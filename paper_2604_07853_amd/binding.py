@@ -22,16 +22,19 @@ E4M3_ACT_FORMATS = (QARL_FP8_E4M3_CH, QARL_FP4_E2M1_CH, QARL_W4A8_G128)   # e4m3
 QARL_PATH_AUTO, QARL_PATH_DECODE, QARL_PATH_PREFILL = 0, 1, 2
 QARL_EPI_NONE, QARL_EPI_SILU_MUL, QARL_EPI_COMBINE = 0, 1, 2
 QARL_OUT_BF16, QARL_OUT_F32 = 0, 1
-QARL_KV_BF16, QARL_KV_E4M3 = 1, 2
+QARL_KV_BF16, QARL_KV_E4M3, QARL_KV_E2M1 = 1, 2, 3
+QARL_ROPE_HALF, QARL_ROPE_PAIRS = 0, 1
+QARL_ROPE_PLAIN, QARL_ROPE_LINEAR, QARL_ROPE_YARN, QARL_ROPE_BANDS = 0, 1, 2, 3
+QARL_ROPE_MAX_PAIRS = 128
 
-# the first ten return a string or a size, the rest a qarl_status
+# the first eleven return a string or a size, the rest a qarl_status
 EXPORTS = ["qarl_last_error", "qarl_add_rmsnorm_backward_workspace_bytes", "qarl_kv_cache_bytes", "qarl_kv_scales_bytes",
-           "qarl_paged_attention_workspace_bytes", "qarl_qgemm_workspace_bytes", "qarl_logprob_workspace_bytes",
+           "qarl_paged_attention_workspace_bytes", "qarl_sample_workspace_bytes", "qarl_qgemm_workspace_bytes", "qarl_logprob_workspace_bytes",
            "qarl_token_logprob_static_limit", "qarl_codes_bytes", "qarl_scales_bytes", "qarl_quantize_weights", "qarl_quantize_rows_fp8", "qarl_moe_route", "qarl_qgemm_grouped",
            "qarl_qgemm_routed", "qarl_moe_layer_routed", "qarl_token_logprob", "qarl_logprob_mismatch", "qarl_tbpo_objective",
            "qarl_token_logprob_static", "qarl_codes_to_canonical", "qarl_qgemm_grouped_dx",
            "qarl_grouped_dw", "qarl_add_rmsnorm", "qarl_add_rmsnorm_backward", "qarl_kv_cache_write", "qarl_kv_cache_read",
-           "qarl_paged_attention"]
+           "qarl_paged_attention", "qarl_rope_frequencies", "qarl_rope_init", "qarl_rotary", "qarl_rotary_kv_write", "qarl_sample"]
 
 
 class QarlError(RuntimeError):
@@ -49,6 +52,10 @@ class qarl_kv_cache(C.Structure):
     _fields_ = [("fmt", C.c_int32), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p),
                 ("v_scales", C.c_void_p)]
+
+
+class qarl_rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("turns", C.c_uint64 * QARL_ROPE_MAX_PAIRS)]
 
 
 _lib = None
@@ -108,9 +115,16 @@ def lib():
         L.qarl_paged_attention_workspace_bytes.argtypes = [C.POINTER(qarl_kv_cache)] + [i32] * 5
         L.qarl_paged_attention.argtypes = [vp, i64, i64, i32, i32, C.POINTER(qarl_kv_cache), vp, i64, i32, vp, vp, i32, i32, i32, f32,
                                            i32, vp, i32, vp, vp, sz, vp]
-        for name in EXPORTS[1:5]:
+        rope = C.POINTER(qarl_rope)
+        L.qarl_rope_frequencies.argtypes = [i32, C.c_double, i32] + [C.c_double] * 4 + [vp, vp]
+        L.qarl_rope_init.argtypes = [rope, i32, i32, vp, f32]
+        L.qarl_rotary.argtypes = [rope, vp, i64, i32, i32] + [vp, i64, i64, i32, vp, i64, i64] * 2 + [i32, vp]
+        L.qarl_rotary_kv_write.argtypes = [C.POINTER(qarl_kv_cache), rope, vp, i64, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp]
+        L.qarl_sample_workspace_bytes.argtypes = [i32, i32]
+        L.qarl_sample.argtypes = [vp, i32, i64, i32, i32] + [vp] * 9 + [sz, vp]
+        for name in EXPORTS[1:6]:
             getattr(L, name).restype = C.c_size_t
-        for name in EXPORTS[10:]:
+        for name in EXPORTS[11:]:
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -543,12 +557,13 @@ def qarl_add_rmsnorm_backward(dy, h, weight, eps, dh=None, dx=None, dw=None, wan
 
 class KVCache:
     """A paged KV cache: the tensors plus the C descriptor.  k, v [num_pages, kv_heads, page_size, head_dim], bf16 or (with k_scales and
-    v_scales, fp32 [num_pages, kv_heads, page_size]) uint8 e4m3 codes."""
+    v_scales, fp32 [num_pages, kv_heads, page_size]) uint8 e4m3 codes; QARL_KV_E2M1: k, v uint8 [num_pages, kv_heads, page_size, head_dim / 2], k_scales
+    and v_scales uint8 [num_pages, kv_heads, page_size, 4]."""
 
     def __init__(self, fmt, k, v, k_scales=None, v_scales=None):
-        if fmt not in (QARL_KV_BF16, QARL_KV_E4M3):
+        if fmt not in (QARL_KV_BF16, QARL_KV_E4M3, QARL_KV_E2M1):
             raise ValueError("unknown cache format %r" % (fmt,))
-        dt = torch.uint8 if fmt == QARL_KV_E4M3 else torch.bfloat16
+        dt = torch.bfloat16 if fmt == QARL_KV_BF16 else torch.uint8
         for t in (k, v):
             if t.dtype != dt or t.dim() != 4 or t.shape != k.shape or not t.is_contiguous():
                 raise ValueError("k and v must be contiguous %s tensors of one shape [pages, heads, page size, head dim]" % dt)
@@ -556,12 +571,19 @@ class KVCache:
             for t in (k_scales, v_scales):
                 if t is None or t.dtype != torch.float32 or t.shape != k.shape[:3] or not t.is_contiguous():
                     raise ValueError("k_scales and v_scales must be contiguous fp32 tensors %s" % list(k.shape[:3]))
-        if any(t.device != k.device for t in ((v, k_scales, v_scales) if fmt == QARL_KV_E4M3 else (v,))):
+        if fmt == QARL_KV_E2M1:
+            for t in (k_scales, v_scales):
+                if t is None or t.dtype != torch.uint8 or t.shape != (*k.shape[:3], 4) or not t.is_contiguous():
+                    raise ValueError("k_scales and v_scales must be contiguous uint8 tensors %s" % [*k.shape[:3], 4])
+        if any(t.device != k.device for t in ((v,) if fmt == QARL_KV_BF16 else (v, k_scales, v_scales))):
             raise ValueError("the buffers of a cache must be on one device")
         self.fmt, self.k, self.v, self.k_scales, self.v_scales = fmt, k, v, k_scales, v_scales
         self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        if fmt == QARL_KV_E2M1:
+            self.head_dim *= 2          # two codes a byte
+        scaled = fmt != QARL_KV_BF16
         self.desc = qarl_kv_cache(fmt, self.num_pages, self.page_size, self.kv_heads, self.head_dim, k.data_ptr(), v.data_ptr(),
-                                  k_scales.data_ptr() if fmt == QARL_KV_E4M3 else None, v_scales.data_ptr() if fmt == QARL_KV_E4M3 else None)
+                                  k_scales.data_ptr() if scaled else None, v_scales.data_ptr() if scaled else None)
         self.ref = C.byref(self.desc)
         self.gpu = k.get_device()       # -1: host memory, which the calls refuse
 
@@ -572,14 +594,20 @@ class KVCache:
             codes = [torch.empty(shape, dtype=torch.uint8, device=device) for _ in range(2)]
             scales = [torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2)]
             return KVCache(fmt, *codes, *scales)
+        if fmt == QARL_KV_E2M1:
+            if head_dim % 2:
+                raise ValueError("two codes of KV_E2M1 share a byte: head_dim must be even (got %d)" % head_dim)
+            codes = [torch.empty((*shape[:3], head_dim // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+            scales = [torch.empty((*shape[:3], 4), dtype=torch.uint8, device=device) for _ in range(2)]
+            return KVCache(fmt, *codes, *scales)
         return KVCache(fmt, *[torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)])
 
 
-def _heads(t, name, shape, gpu):
-    """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose heads are contiguous."""
+def _heads(t, name, shape, gpu, dtype=_BF16):
+    """(pointer, token stride, head stride) of a [tokens, heads, head_dim] view whose heads are contiguous."""
     token, head, last = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.shape != shape or t.dtype is not _BF16 or t.get_device() != gpu or gpu < 0 or last != 1:
-        _wrong(t, name, "%s %s with contiguous heads" % (list(shape), _BF16), gpu)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != gpu or gpu < 0 or last != 1:
+        _wrong(t, name, "%s %s with contiguous heads" % (list(shape), dtype), gpu)
     return t.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0      # (the stride of a single one may be anything)
 
 
@@ -598,6 +626,75 @@ def qarl_kv_cache_write(cache, k, v, slots):
     kp, kt, kh = _heads(k, "k", shape, gpu)
     vp, vt, vh = _heads(v, "v", shape, gpu)
     _check(lib().qarl_kv_cache_write(_cache(cache, gpu), kp, kt, kh, vp, vt, vh, T, _flat(slots, "slots", _I64, (T,), gpu), _raw_stream(gpu)))
+
+
+def qarl_rope_frequencies(rotary_dim, base=10000.0, scaling=QARL_ROPE_PLAIN, factor=1.0, original_len=1.0, low=1.0, high=32.0):
+    """(frequencies, a list of rotary_dim / 2 numbers in radians a position, and the amplitude); see include/qarl.h."""
+    f, amplitude = (C.c_double * max(1, rotary_dim // 2))(), C.c_float()
+    _check(lib().qarl_rope_frequencies(rotary_dim, base, scaling, factor, original_len, low, high, f, C.byref(amplitude)))
+    return list(f), amplitude.value
+
+
+class Rope:
+    """Rotary positions of rotary_dim elements of a head: the C descriptor.  Frequencies by base and scaling (qarl_rope_frequencies), or any others as
+    `frequencies` (radians a position); amplitude: what the turned pairs are multiplied by, instead of the scaling's own."""
+
+    def __init__(self, rotary_dim, base=10000.0, layout=QARL_ROPE_HALF, scaling=QARL_ROPE_PLAIN, factor=1.0, original_len=1.0, low=1.0, high=32.0,
+                 frequencies=None, amplitude=None):
+        if frequencies is None:
+            frequencies, own = qarl_rope_frequencies(rotary_dim, base, scaling, factor, original_len, low, high)
+        else:
+            own = 1.0
+            if len(frequencies) * 2 != rotary_dim:
+                raise ValueError("frequencies must be %d numbers (got %d)" % (rotary_dim // 2, len(frequencies)))
+        self.rotary_dim, self.layout, self.frequencies = rotary_dim, layout, [float(f) for f in frequencies]
+        self.amplitude = own if amplitude is None else amplitude
+        self.desc = qarl_rope()
+        _check(lib().qarl_rope_init(C.byref(self.desc), rotary_dim, layout, (C.c_double * len(self.frequencies))(*self.frequencies), self.amplitude))
+        self.ref = C.byref(self.desc)
+
+
+def _turned(t, out, name, dtype, T, D, gpu):
+    """(out, pointer, token stride, head stride, heads, out's three) of the heads of one side of a rotation."""
+    if t is None:
+        if out is not None:
+            raise ValueError("%s_out without %s" % (name, name))
+        return None, (None, 0, 0, 0, None, 0, 0)
+    shape = (T, t.shape[1] if t.dim() == 3 else -1, D)
+    if out is None:
+        out = torch.empty(t.shape, dtype=dtype, device=t.device)
+    xp, xt, xh = _heads(t, name, shape, gpu, dtype)
+    yp, yt, yh = _heads(out, name + "_out", shape, gpu, dtype)
+    return out, (xp, xt, xh, shape[1], yp, yt, yh)
+
+
+def qarl_rotary(rope, positions, q, k=None, inverse=False, q_out=None, k_out=None):
+    """q [T, heads, head_dim] and k [T, kv_heads, head_dim] (bf16 or fp32, both of one type, any token and head stride; k may be None) turned to their
+    positions [T] (int64), or back (inverse: the gradient); see include/qarl.h.  q_out and k_out may be q and k.  Returns dict(q, k)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens, heads, head_dim] (got %s)" % list(q.shape))
+    T, _, D = q.shape
+    gpu = q.get_device()
+    dt = _F32 if q.dtype is _F32 else _BF16
+    k_out, ka = _turned(k, k_out, "k", dt, T, D, gpu)
+    q_out, qa = _turned(q, q_out, "q", dt, T, D, gpu)
+    _check(lib().qarl_rotary(rope.ref, _flat(positions, "positions", _I64, (T,), gpu), T, D, QARL_OUT_F32 if dt is _F32 else QARL_OUT_BF16, *qa, *ka,
+                             int(bool(inverse)), _raw_stream(gpu)))
+    return dict(q=q_out, k=k_out)
+
+
+def qarl_rotary_kv_write(cache, rope, positions, q, k, v, slots, q_out=None):
+    """Turns q [T, heads, head_dim] (may be None) and k [T, kv_heads, head_dim] to their positions [T] (int64) and writes k and v into the slots [T]
+    (int64) of the cache; see include/qarl.h.  bf16, any token and head stride; q_out may be q.  Returns the turned q."""
+    T = slots.numel()
+    D, gpu = cache.head_dim, k.get_device()
+    shape = (T, cache.kv_heads, D)
+    q_out, qa = _turned(q, q_out, "q", _BF16, T, D, gpu)
+    kp, kt, kh = _heads(k, "k", shape, gpu)
+    vp, vt, vh = _heads(v, "v", shape, gpu)
+    _check(lib().qarl_rotary_kv_write(_cache(cache, gpu), rope.ref, _flat(positions, "positions", _I64, (T,), gpu), T, *qa, kp, kt, kh, vp, vt, vh,
+                                      _flat(slots, "slots", _I64, (T,), gpu), _raw_stream(gpu)))
+    return q_out
 
 
 def qarl_kv_cache_read(cache, block_table, offsets, total, out=None):
@@ -644,3 +741,36 @@ def qarl_paged_attention(query, cache, block_table, kv_lens, q_offsets, max_q_le
                                   QARL_OUT_F32 if f32 else QARL_OUT_BF16, None if lse is None else _flat(lse, "lse", _F32, (T, Hq), gpu), wsp, wsn,
                                   _raw_stream(gpu)))
     return dict(out=out, lse=lse)
+
+
+def qarl_sample_workspace_bytes(T, V):
+    return lib().qarl_sample_workspace_bytes(T, V)
+
+
+def qarl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, kept_logprob=None, want_kept=False, ws=None):
+    """A token for each row of logits [T, V] (bf16 or fp32, rows at any stride) from one random number u [T] each; see include/qarl.h.  temperature, top_p,
+    min_p fp32 [T], top_k int32 [T], or None.  Allocates token (int32), logprob, kept_logprob (want_kept) and ws when not given.
+    Returns dict(token, logprob, kept_logprob)."""
+    T, V = logits.shape
+    dev, gpu = logits.device, logits.get_device()
+    dt, code = (_F32, QARL_OUT_F32) if logits.dtype is _F32 else (_BF16, QARL_OUT_BF16)
+    row = (T,)
+    if token is None:
+        token = torch.empty(row, dtype=_I32, device=dev)
+    if logprob is None:
+        logprob = torch.empty(row, dtype=_F32, device=dev)
+    if kept_logprob is None and want_kept:
+        kept_logprob = torch.empty(row, dtype=_F32, device=dev)
+    lp, stride = _rows(logits, "logits", dt, (T, V), gpu)
+    L = lib()
+    if ws is None:
+        need = L.qarl_sample_workspace_bytes(T, V)
+        if need:
+            ws = torch.empty((need,), dtype=_U8, device=dev)
+    wsp, wsn = _ws(ws, gpu)
+    _check(L.qarl_sample(lp, code, stride, T, V, _flat(u, "u", _F32, row, gpu), None if temperature is None else _flat(temperature, "temperature", _F32, row, gpu),
+                         None if top_k is None else _flat(top_k, "top_k", _I32, row, gpu), None if top_p is None else _flat(top_p, "top_p", _F32, row, gpu),
+                         None if min_p is None else _flat(min_p, "min_p", _F32, row, gpu), _flat(token, "token", _I32, row, gpu),
+                         _flat(logprob, "logprob", _F32, row, gpu), None if kept_logprob is None else _flat(kept_logprob, "kept_logprob", _F32, row, gpu),
+                         wsp, wsn, _raw_stream(gpu)))
+    return dict(token=token, logprob=logprob, kept_logprob=kept_logprob)

@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqarl.so")
 SOURCES = ["api.hip", "quantize.hip", "route.hip", "qgemm_stream_fp8.hip", "qgemm_stream_fp4.hip", "qgemm_stream_w4.hip", "qgemm_small_w4.hip", "qgemm_small_fp8.hip", "qgemm_tile.hip", "qgemm_backward.hip",
            "qgemm_tile_fp8.hip", "combine.hip", "logprob.hip", "tbpo.hip",
-           "api_attention.hip", "rmsnorm.hip", "kv_cache.hip", "attention.hip", "attention_few.hip",
+           "api_attention.hip", "rmsnorm.hip", "rotary.hip", "kv_cache.hip", "sample.hip", "attention.hip", "attention_few.hip",
            "attention_tile.hip"]
 # packed fp32 operations are switched off for all device code
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",

@@ -14,24 +14,26 @@ namespace qarl {
 
 constexpr int kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 
-template <int D, bool E4M3>
+template <int D, int FMT>
 struct FewLayout {
-    static constexpr int kRowBytes = D * (E4M3 ? 1 : 2);
+    static constexpr bool E4M3 = FMT == QARL_KV_E4M3, E2M1 = FMT == QARL_KV_E2M1;
+    static constexpr int kRowBytes = E2M1 ? D / 2 : E4M3 ? D : 2 * D;
     static constexpr int kChunks = kRowBytes / 16;                       // 16-byte chunks of a row
     static constexpr int kRowsPerCopy = 1024 / kRowBytes;                // an asynchronous copy moves 64 x 16 bytes
     static constexpr int kCopies = kFewTile / kRowsPerCopy;              // per tile of keys, and of values
     static constexpr int kHalf = kFewTile * kRowBytes;                   // bytes of a tile of keys
-    static constexpr int kStage = 2 * kHalf + (E4M3 ? 256 : 0);          // keys, values, 32 + 32 scales
-    static constexpr int kStageCopies = 2 * kCopies + (E4M3 ? 1 : 0);
+    static constexpr int kStage = 2 * kHalf + (E4M3 || E2M1 ? 256 : 0);  // keys, values, 32 + 32 scales (e2m1: four bytes each)
+    static constexpr int kStageCopies = 2 * kCopies + (E4M3 || E2M1 ? 1 : 0);
     static constexpr int kRing = kStage <= 5000 ? 4 : 2;                 // stages; about 64 KiB per workgroup, D = 128 in bf16 128
     // Chunk c of row r lies at chunk c ^ swz(r): 16 rows that are read at the same chunk spread over all banks
     __device__ static constexpr int swz(int r) { return (r / (256 / kRowBytes)) & (kChunks - 1); }
 };
 
-template <int D, bool E4M3, int NR>
+template <int D, int FMT, int NR>
 __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_kernel(AttnArgs a, int chunk, AttnParts parts)
 {
-    using L = FewLayout<D, E4M3>;
+    using L = FewLayout<D, FMT>;
+    constexpr bool E4M3 = L::E4M3, E2M1 = L::E2M1;
     constexpr int KS = D / 32, DT = D / 16;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -66,7 +68,8 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
         const int page = table[pos >> shift];
         pages[i] = page >= 0 && page < a.kv.num_pages ? page : -1;
     }
-    // the queries: B operand, lane holds row n = lane & 15, eight of D at 8 q (bf16 cache) or as the keys' 16-byte reads order them (e4m3)
+    // the queries: B operand, lane holds row n = lane & 15, eight of D at 8 q (bf16 cache) or as the keys' 16-byte reads order them (e4m3; e2m1: a lane's
+    // keys are the q-th quarter of a row, which has one scale)
     bf16x8 qf[NR][KS];
     int see_lo[NR], see_hi[NR];
 #pragma unroll
@@ -76,7 +79,7 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
         const uint16_t *qp = (const uint16_t *)a.q + (int64_t)(sr.row_lo + i) * a.q_token_stride + (int64_t)(h * G + (row < R ? g : 0)) * a.q_head_stride;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const int d = E4M3 ? 64 * (ks >> 1) + 16 * q + 8 * (ks & 1) : 32 * ks + 8 * q;
+            const int d = E2M1 ? D / 4 * q + 8 * ks : E4M3 ? 64 * (ks >> 1) + 16 * q + 8 * (ks & 1) : 32 * ks + 8 * q;
             qf[r][ks] = __builtin_bit_cast(bf16x8, *(const u32x4 *)(qp + d));
         }
         if (row >= R) see_hi[r] = -1;
@@ -100,13 +103,14 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             const int logical = (lane % L::kChunks) ^ L::swz(r);
             int page;
             if (L::kRowsPerCopy <= 8) page = __builtin_amdgcn_readlane(pl, c * L::kRowsPerCopy);
-            else page = lane < 32 ? __builtin_amdgcn_readlane(pl, c * 16) : __builtin_amdgcn_readlane(pl, c * 16 + 8);
+            else if (L::kRowsPerCopy == 16) page = lane < 32 ? __builtin_amdgcn_readlane(pl, c * 16) : __builtin_amdgcn_readlane(pl, c * 16 + 8);
+            else page = pages[t * 4 + (lane >> 4)];
             const int64_t first = ((int64_t)max(page, 0) * Hkv + h) << shift;
             const uint32_t in = (uint32_t)(min(max(pos0 + r, begin), end - 1) & ((1 << shift) - 1)) * (uint32_t)L::kRowBytes + (uint32_t)(logical * 16);
             copy16_to_lds((const char *)a.kv.k + first * L::kRowBytes + in, to + c * 1024);
             copy16_to_lds((const char *)a.kv.v + first * L::kRowBytes + in, to + L::kHalf + c * 1024);
         }
-        if (E4M3) {
+        if (E4M3 || E2M1) {
             const int64_t at = (((int64_t)max(pl, 0) * Hkv + h) << shift) + (min(max(pos0 + (lane & 31), begin), end - 1) & ((1 << shift) - 1));
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((lane < 32 ? a.kv.k_scales : a.kv.v_scales) + at),
                                              (__attribute__((address_space(3))) void *)(to + 2 * L::kHalf), 4, 0, 0);
@@ -155,7 +159,22 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
 #pragma unroll
             for (int n = 0; n < NR; ++n) z[u][n] = f32x4{0.f, 0.f, 0.f, 0.f};
             const char *kr = st + r * L::kRowBytes;
-            if (E4M3) {
+            if (E2M1) {
+                const float sc = e2m1_scale(((const uint8_t *)(st + 2 * L::kHalf))[r * 4 + q]);
+                u32x4 w;
+                if (D == 128) {
+                    w = *(const u32x4 *)(kr + ((q ^ L::swz(r)) * 16));
+                } else {
+                    const u32x2 half = *(const u32x2 *)(kr + (((q >> 1) ^ L::swz(r)) * 16) + (q & 1) * 8);
+                    w = u32x4{half[0], half[1], 0, 0};
+                }
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const bf16x8 k = __builtin_bit_cast(bf16x8, widen_e2m1x8(w[ks], sc));
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) z[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[n][ks], z[u][n], 0, 0, 0);
+                }
+            } else if (E4M3) {
 #pragma unroll
                 for (int kp = 0; kp < KS / 2; ++kp) {
                     const u32x4 w = *(const u32x4 *)(kr + (((4 * kp + q) ^ L::swz(r)) * 16));
@@ -176,8 +195,10 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             }
         }
         f32x4 vs[2];
+        u32x4 vb[2];        // e2m1: the four scales of a value's row, a byte each
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            if (E2M1) vb[u] = *(const u32x4 *)(st + 2 * L::kHalf + 128 + (u * 16 + 4 * q) * 4);
             f32x4 kscale = f32x4{c2, c2, c2, c2};
             if (E4M3) {
                 kscale = *(const f32x4 *)(st + 2 * L::kHalf + (u * 16 + 4 * q) * 4) * c2;
@@ -240,7 +261,7 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
                 u32x4 v = *w;
                 const u32x4 was = v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = E4M3 ? only_finite_e4m3(v[e]) : only_finite_bf16(v[e]);
+                for (int e = 0; e < 4; ++e) v[e] = E2M1 ? v[e] : E4M3 ? only_finite_e4m3(v[e]) : only_finite_bf16(v[e]);   // (e2m1 codes are finite)
                 if (v[0] != was[0] || v[1] != was[1] || v[2] != was[2] || v[3] != was[3]) {
                     *w = v;
                     bad = true;
@@ -254,6 +275,14 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
                         bad = true;
                     }
             }
+            if (E2M1) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t fine = no_nan_scales(vb[e >> 2][e & 3]);
+                    bad |= fine != vb[e >> 2][e & 3];
+                    vb[e >> 2][e & 3] = fine;
+                }
+            }
             rare |= __ballot(bad) != 0;
         }
 #pragma unroll
@@ -264,6 +293,49 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             }
             pf[n] = pack_bf16x8(pv[n]);
         }
+        if (E2M1) {
+            // A row's four quarters have scales of their own, which the probabilities take on: exact (powers of two), rounded to bf16 once as before.  A
+            // transposing read brings a lane its eight positions of two runs of 16 of D.
+            const int r = (m16 & 3) + 4 * q + 4 * (m16 & 4);
+            const uint32_t at = (uint32_t)(uintptr_t)(LdsPtr)st + L::kHalf + r * L::kRowBytes + (L::swz(r) * 16) + (m16 >> 3) * 8;
+            u32x2 w[L::kChunks];
+            if (D == 128) {
+                asm volatile("ds_read_b64_tr_b4 %0, %4\n\tds_read_b64_tr_b4 %1, %5\n\tds_read_b64_tr_b4 %2, %6\n\tds_read_b64_tr_b4 %3, %7\n\t"
+                             "s_waitcnt lgkmcnt(0)"
+                             : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[L::kChunks - 2]), "=&v"(w[L::kChunks - 1])
+                             : "v"(at), "v"(at ^ 16), "v"(at ^ 32), "v"(at ^ 48)
+                             : "memory");
+            } else {
+                asm volatile("ds_read_b64_tr_b4 %0, %2\n\tds_read_b64_tr_b4 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(w[0]), "=&v"(w[1])
+                             : "v"(at), "v"(at ^ 16)
+                             : "memory");
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float sc[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t b = (vb[e >> 2][e & 3] >> (8 * g)) & 0xffu;
+                    sc[e] = b == 255 ? __builtin_nanf("") : e2m1_scale(b);
+                }
+                bf16x8 pg[NR];
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    float t[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) t[e] = pv[n][e] * sc[e];
+                    pg[n] = pack_bf16x8(t);
+                }
+#pragma unroll
+                for (int x = 0; x < DT / 4; ++x) {      // the runs of 16 of D of this quarter
+                    const int dt = g * (DT / 4) + x;
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, widen_e2m1x8(w[dt >> 1][dt & 1], 1.0f));
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) acc[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pg[n], acc[n][dt], 0, 0, 0);
+                }
+            }
+        } else
         // (the reads and their wait in one block: the compiler would let a transposing read that it can see wait for the copies in flight)
 #pragma unroll
         for (int d4 = 0; d4 < DT; d4 += 4) {
@@ -282,7 +354,7 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             } else {
                 const int r = 4 * q + (m16 >> 2);
                 const uint32_t at = (uint32_t)(uintptr_t)(LdsPtr)st + L::kHalf + r * L::kRowBytes + ((((m16 & 3) >> 1) ^ L::swz(r)) * 16) + (m16 & 1) * 8;
-                static_assert(E4M3 || L::swz(16) == 0, "positions 16 apart lie at the same chunk");
+                static_assert(FMT != QARL_KV_BF16 || L::swz(16) == 0, "positions 16 apart lie at the same chunk");
                 u32x2 w[8];
                 asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\tds_read_b64_tr_b16 %2, %9\n\t"
                              "ds_read_b64_tr_b16 %3, %9 offset:%12\n\tds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
@@ -317,7 +389,7 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int64_t d = at * D + 16 * dt + 4 * q + e;
-                        const float v = E4M3 ? sc * __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)a.kv.v)[d], 0) : bf16_bits_to_f32(((const uint16_t *)a.kv.v)[d]);
+                        const float v = E2M1 ? (a.kv.v_bytes()[at * 4 + dt / (DT / 4)] == 255 ? __builtin_nanf("") : 0.f) : E4M3 ? sc * __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)a.kv.v)[d], 0) : bf16_bits_to_f32(((const uint16_t *)a.kv.v)[d]);
                         const bool bad = !(fabsf(v) < __builtin_inff());
 #pragma unroll
                         for (int n = 0; n < NR; ++n)
@@ -377,10 +449,10 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
     }
 }
 
-template <int D, bool E4M3, int NR>
+template <int D, int FMT, int NR>
 static int launch_few_as(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
 {
-    using L = FewLayout<D, E4M3>;
+    using L = FewLayout<D, FMT>;
     static LdsLimitOnce once;
     const int64_t grid = (int64_t)a.S * a.kv.kv_heads * p.few_splits;
     if (grid > 0x7fffffffLL) {
@@ -388,25 +460,31 @@ static int launch_few_as(const AttnArgs &a, const AttnPlan &p, const AttnParts &
         return QARL_ERR_UNSUPPORTED;
     }
     const int stream = kFewWaves * L::kRing * L::kStage + p.few_chunk / 8 * 4, join = kFewWaves * 16 * NR * (D + 4 + 2) * 4;
-    int rc = raise_lds_limit((const void *)attention_few_kernel<D, E4M3, NR>, once, "attention_few_kernel");
+    int rc = raise_lds_limit((const void *)attention_few_kernel<D, FMT, NR>, once, "attention_few_kernel");
     if (rc) return rc;
-    attention_few_kernel<D, E4M3, NR><<<dim3((unsigned)grid), dim3(kFewThreads), stream > join ? stream : join, s>>>(a, p.few_chunk, parts);
+    attention_few_kernel<D, FMT, NR><<<dim3((unsigned)grid), dim3(kFewThreads), stream > join ? stream : join, s>>>(a, p.few_chunk, parts);
     return check_hip(hipGetLastError(), "attention_few_kernel");
 }
 
-template <int D, bool E4M3>
+template <int D, int FMT>
 static int launch_few_rows(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
 {
-    if (p.few_nr == 1) return launch_few_as<D, E4M3, 1>(a, p, parts, s);
-    if (p.few_nr == 2) return launch_few_as<D, E4M3, 2>(a, p, parts, s);
-    return launch_few_as<D, E4M3, 4>(a, p, parts, s);
+    if (p.few_nr == 1) return launch_few_as<D, FMT, 1>(a, p, parts, s);
+    if (p.few_nr == 2) return launch_few_as<D, FMT, 2>(a, p, parts, s);
+    return launch_few_as<D, FMT, 4>(a, p, parts, s);
+}
+
+template <int D>
+static int launch_few_format(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
+{
+    if (a.kv.fmt == QARL_KV_E4M3) return launch_few_rows<D, QARL_KV_E4M3>(a, p, parts, s);
+    if (a.kv.fmt == QARL_KV_E2M1) return launch_few_rows<D, QARL_KV_E2M1>(a, p, parts, s);
+    return launch_few_rows<D, QARL_KV_BF16>(a, p, parts, s);
 }
 
 int launch_attention_few(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
 {
-    const bool e4m3 = a.kv.fmt == QARL_KV_E4M3;
-    if (a.kv.head_dim == 128) return e4m3 ? launch_few_rows<128, true>(a, p, parts, s) : launch_few_rows<128, false>(a, p, parts, s);
-    return e4m3 ? launch_few_rows<64, true>(a, p, parts, s) : launch_few_rows<64, false>(a, p, parts, s);
+    return a.kv.head_dim == 128 ? launch_few_format<128>(a, p, parts, s) : launch_few_format<64>(a, p, parts, s);
 }
 
 }  // namespace qarl

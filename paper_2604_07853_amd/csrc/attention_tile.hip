@@ -37,10 +37,11 @@ struct ManyLayout {
     __device__ static constexpr int at_v(int pos) { return (pos & 0x33) | (pos & 4) << 1 | (pos & 8) >> 1; }
 };
 
-template <int D, bool E4M3>
+template <int D, int FMT>
 __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArgs a, int few_rows, int chunk, int blocks, AttnParts parts)
 {
     using L = ManyLayout<D>;
+    constexpr bool E4M3 = FMT == QARL_KV_E4M3, E2M1 = FMT == QARL_KV_E2M1;
     constexpr int KS = D / 16, DT = D / 32;
     extern __shared__ __align__(128) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -170,35 +171,46 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
     // ---- a tile's way from the cache through registers into LDS.
     // Keys: a thread moves 16-byte pieces, kStep positions apart; the 4, 8 or 16 neighbouring positions of a wavefront's load lie in one page, or each
     // eight of them do.  Values: a thread takes eight of D at two neighbouring positions and stores them as eight pairs; a wavefront's positions are 8 or 16.
-    constexpr int kPieces = D * (E4M3 ? 1 : 2) / 16;                   // 16-byte pieces of a row of the cache
+    constexpr int kPieces = (E2M1 ? D / 2 : E4M3 ? D : 2 * D) / 16;    // 16-byte pieces of a row of the cache
     constexpr int kPer = 64 / kPieces, kLoads = kManyTile * kPieces > kManyThreads ? kManyTile * kPieces / kManyThreads : 1, kStep = kManyWaves * kPer;
-    constexpr bool kHalfBusy = kManyTile * kPieces < kManyThreads;     // (e4m3, D = 64: four of the eight wavefronts)
+    constexpr int kBusy = kManyTile * kPieces < kManyThreads ? kManyTile * kPieces / 64 : kManyWaves;      // wavefronts that move keys (e4m3, D = 64, and e2m1: not all)
     constexpr int kEights = D / 8, kVPer = 2 * 64 / kEights;           // positions of a wavefront's load of values
     const int k_row = wave * kPer + lane / kPieces, k_piece = lane % kPieces;
     const int v_row = wave * kVPer + lane / kEights * 2, v_d = lane % kEights * 8;
     struct Staged {
         u32x4 k[kLoads], v[2];
         float scale;
+        uint32_t k_scale, v_scale[2];       // e2m1: bytes
     };
     auto row_page = [&](int page, int first, int per) -> int {        // the page of this lane's row of a wavefront's `per` positions from `first` on
         const int pg = __builtin_amdgcn_readlane(page, first & (kManyTile - 1));
         const int second = __builtin_amdgcn_readlane(page, (first + 8) & (kManyTile - 1));
-        return per > 8 && lane >= 32 ? second : pg;
+        if (per <= 16) return per > 8 && lane >= 32 ? second : pg;
+        const int third = __builtin_amdgcn_readlane(page, (first + 16) & (kManyTile - 1)), fourth = __builtin_amdgcn_readlane(page, (first + 24) & (kManyTile - 1));
+        return lane < 32 ? (lane < 16 ? pg : second) : (lane < 48 ? third : fourth);
     };
     auto load = [&](int tk, int page_k, int tv, int page_v, Staged &st) {
-        if (!kHalfBusy || wave < kManyWaves / 2) {
+        if (kBusy == kManyWaves || wave < kBusy) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const uint32_t in = (uint32_t)in_page(lo + tk * kManyTile + k_row + i * kStep) * (uint32_t)(kPieces * 16) + (uint32_t)(k_piece * 16);
-                st.k[i] = *(const u32x4 *)((const char *)a.kv.k + head_page(row_page(page_k, i * kStep + wave * kPer, kPer)) * (kPieces * 16) + in);
+                const int64_t first = head_page(row_page(page_k, i * kStep + wave * kPer, kPer));
+                st.k[i] = *(const u32x4 *)((const char *)a.kv.k + first * (kPieces * 16) + in);
+                if (E2M1) {     // the scales of a piece: one (D = 128), or two
+                    const uint8_t *sc = a.kv.k_bytes() + (first + in_page(lo + tk * kManyTile + k_row)) * 4 + k_piece * (4 / kPieces);
+                    st.k_scale = D == 128 ? (uint32_t)*sc : (uint32_t)*(const uint16_t *)sc;
+                }
             }
         }
         if (D == 128 || wave < kManyWaves / 2) {
             const char *first = (const char *)a.kv.v + head_page(row_page(page_v, wave * kVPer, kVPer)) * (kPieces * 16);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t in = (uint32_t)in_page(lo + tv * kManyTile + v_row + i) * (uint32_t)(kPieces * 16) + (uint32_t)(v_d * (E4M3 ? 1 : 2));
-                if (E4M3) {
+                const uint32_t in = (uint32_t)in_page(lo + tv * kManyTile + v_row + i) * (uint32_t)(kPieces * 16) + (uint32_t)(E2M1 ? v_d / 2 : E4M3 ? v_d : 2 * v_d);
+                if (E2M1) {
+                    st.v[i][0] = *(const uint32_t *)(first + in);
+                    st.v_scale[i] = a.kv.v_bytes()[(head_page(row_page(page_v, wave * kVPer, kVPer)) + in_page(lo + tv * kManyTile + v_row + i)) * 4 + v_d / (D / 4)];
+                } else if (E4M3) {
                     const u32x2 w = *(const u32x2 *)(first + in);
                     st.v[i][0] = w[0];
                     st.v[i][1] = w[1];
@@ -211,12 +223,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
         if (E4M3 && wave == 1) st.scale = a.kv.v_scales[head_page(page_v) + in_page(lo + tv * kManyTile + lane)];
     };
     auto store_k = [&](int slot, const Staged &st) {
-        if (!kHalfBusy || wave < kManyWaves / 2) {
+        if (kBusy == kManyWaves || wave < kBusy) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int r = k_row + i * kStep;
                 char *to = lds_k + slot * L::kHalf + r * L::kRowBytes;
-                if (E4M3) {
+                if (E2M1) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *(u32x4 *)(to + (((4 * k_piece + c) ^ L::swz_k(r)) * 16)) = widen_e2m1x8(st.k[i][c], e2m1_scale(D == 128 ? st.k_scale : (st.k_scale >> (c >> 1) * 8) & 0xffu));
+                } else if (E4M3) {
                     *(bf16x8 *)(to + (((2 * k_piece) ^ L::swz_k(r)) * 16)) = widen_e4m3x8(st.k[i][0], st.k[i][1]);
                     *(bf16x8 *)(to + (((2 * k_piece + 1) ^ L::swz_k(r)) * 16)) = widen_e4m3x8(st.k[i][2], st.k[i][3]);
                 } else {
@@ -233,7 +249,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
         if (D == 128 || wave < kManyWaves / 2) {
             u32x4 w[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) w[i] = E4M3 ? __builtin_bit_cast(u32x4, widen_e4m3x8(st.v[i][0], st.v[i][1])) : st.v[i];
+            for (int i = 0; i < 2; ++i)
+                w[i] = E2M1 ? widen_e2m1x8(st.v[i][0], e2m1_scale(st.v_scale[i])) : E4M3 ? __builtin_bit_cast(u32x4, widen_e4m3x8(st.v[i][0], st.v[i][1])) : st.v[i];
             if (partly) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -455,7 +472,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int64_t d = at * D + 32 * dt + 8 * (e >> 2) + 4 * half + (e & 3);
-                    const float v = E4M3 ? vs * __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)a.kv.v)[d], 0) : bf16_bits_to_f32(((const uint16_t *)a.kv.v)[d]);
+                    const float v = E2M1 ? (a.kv.v_bytes()[at * 4 + (32 * dt + 8 * (e >> 2)) / (D / 4)] == 255 ? __builtin_nanf("") : 0.f)
+                                    : E4M3 ? vs * __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)a.kv.v)[d], 0) : bf16_bits_to_f32(((const uint16_t *)a.kv.v)[d]);
                     const bool bad = !(fabsf(v) < __builtin_inff());
                     if (bad && j >= see_lo && j <= see_hi) acc[dt][e] += v;
                 }
@@ -503,7 +521,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attention_tile_kernel(AttnArg
     }
 }
 
-template <int D, bool E4M3>
+template <int D, int FMT>
 static int launch_tile_as(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
 {
     static LdsLimitOnce once;
@@ -512,17 +530,23 @@ static int launch_tile_as(const AttnArgs &a, const AttnPlan &p, const AttnParts 
         set_error("qarl_paged_attention: %lld row blocks exceed the grid limit", (long long)grid);
         return QARL_ERR_UNSUPPORTED;
     }
-    int rc = raise_lds_limit((const void *)attention_tile_kernel<D, E4M3>, once, "attention_tile_kernel");
+    int rc = raise_lds_limit((const void *)attention_tile_kernel<D, FMT>, once, "attention_tile_kernel");
     if (rc) return rc;
-    attention_tile_kernel<D, E4M3><<<dim3((unsigned)grid), dim3(kManyThreads), ManyLayout<D>::kLds, s>>>(a, 16 * p.few_nr, p.tile_chunk, p.tile_blocks, parts);
+    attention_tile_kernel<D, FMT><<<dim3((unsigned)grid), dim3(kManyThreads), ManyLayout<D>::kLds, s>>>(a, 16 * p.few_nr, p.tile_chunk, p.tile_blocks, parts);
     return check_hip(hipGetLastError(), "attention_tile_kernel");
+}
+
+template <int D>
+static int launch_tile_format(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
+{
+    if (a.kv.fmt == QARL_KV_E4M3) return launch_tile_as<D, QARL_KV_E4M3>(a, p, parts, s);
+    if (a.kv.fmt == QARL_KV_E2M1) return launch_tile_as<D, QARL_KV_E2M1>(a, p, parts, s);
+    return launch_tile_as<D, QARL_KV_BF16>(a, p, parts, s);
 }
 
 int launch_attention_tile(const AttnArgs &a, const AttnPlan &p, const AttnParts &parts, hipStream_t s)
 {
-    const bool e4m3 = a.kv.fmt == QARL_KV_E4M3;
-    if (a.kv.head_dim == 128) return e4m3 ? launch_tile_as<128, true>(a, p, parts, s) : launch_tile_as<128, false>(a, p, parts, s);
-    return e4m3 ? launch_tile_as<64, true>(a, p, parts, s) : launch_tile_as<64, false>(a, p, parts, s);
+    return a.kv.head_dim == 128 ? launch_tile_format<128>(a, p, parts, s) : launch_tile_format<64>(a, p, parts, s);
 }
 
 }  // namespace qarl

@@ -194,6 +194,45 @@ struct LaneScale {
     }
 };
 
+// The 4-bit quantizer of the KV cache: e2m1 codes (alpha = 6) of a group of values under the smallest power of two whose sixfold reaches the group's absmax,
+// 2^-100 to 2^125, stored as its exponent + 127 (255 for a group with an infinity or a NaN: it reads as NaN).  absmax as LaneScale::absmax8 makes it.
+// v_cvt_scalef32_pk_fp4_f32 divides by the power of two exactly and rounds to nearest even, saturating (checked on gfx950 against a software encoder, ties
+// and scales at both ends included); the way back, v_cvt_scalef32_pk_bf16_fp4, is exact for all 255 scales, and a NaN under the scale +inf that byte 255 becomes.
+struct E2m1Scale {
+    uint8_t byte;
+    float s;
+    __device__ __forceinline__ explicit E2m1Scale(float absmax)
+    {
+        const uint32_t u = __float_as_uint(absmax);
+        const int e = (int)(u >> 23) - ((u & 0x7fffffu) <= 0x400000u ? 2 : 1);      // absmax = 1.m 2^x <= 1.5 2^(e + 2)
+        const int b = absmax < __builtin_inff() ? min(max(e, 27), 252) : 255;
+        byte = (uint8_t)b;
+        s = __uint_as_float((uint32_t)b << 23);
+    }
+    // eight codes, the first in the lowest bits
+    __device__ __forceinline__ uint32_t quantize8(const float (&x)[8]) const
+    {
+        if (byte == 255) return 0;
+        uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], s, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+    }
+};
+__device__ __forceinline__ float e2m1_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight e2m1 codes times their scale -> bf16 (exact)
+__device__ __forceinline__ u32x4 widen_e2m1x8(uint32_t w, float scale)
+{
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    u32x4 o;
+    o[0] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+    o[1] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+    o[2] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+    o[3] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    return o;
+}
+
 __device__ __forceinline__ void bf16x8_to_f32(u32x4 v, float (&t)[8])
 {
 #pragma unroll
@@ -506,12 +545,53 @@ struct KvArgs {
     int fmt;
     int num_pages, page_shift, kv_heads, head_dim;   // page_size = 1 << page_shift
     void *k, *v;
-    float *k_scales, *v_scales;
+    float *k_scales, *v_scales;                      // KV_E2M1: four bytes a row
+    __host__ __device__ const uint8_t *k_bytes() const { return (const uint8_t *)k_scales; }
+    __host__ __device__ const uint8_t *v_bytes() const { return (const uint8_t *)v_scales; }
 };
 int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, const void *v, int64_t vts, int64_t vhs, int64_t T,
                     const int64_t *slots, hipStream_t s);
 int launch_kv_read(const KvArgs &c, const int32_t *table, int64_t table_stride, int table_width, const int32_t *offsets, int S,
                    int64_t total, void *k_out, void *v_out, hipStream_t s);
+// Rotary positions (rotary.hip)
+struct RotHeads {
+    const void *in;          // [T][heads][head_dim] at these strides (elements)
+    int64_t token_stride, head_stride;
+    void *out;
+    int64_t out_token_stride, out_head_stride;
+    int heads;
+};
+struct RotaryArgs {
+    qarl_rope rope;
+    const int64_t *positions;
+    int64_t T;
+    int head_dim, f32, inverse;
+    RotHeads q, k;
+};
+int launch_rotary(const RotaryArgs &a, hipStream_t s);
+struct RotaryWriteArgs {
+    qarl_rope rope;
+    const int64_t *positions, *slots;
+    int64_t T;
+    KvArgs kv;
+    RotHeads q;
+    const void *k, *v;
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+};
+int launch_rotary_write(const RotaryWriteArgs &a, hipStream_t s);
+struct SampleArgs {
+    const void *logits;
+    int f32;
+    int64_t stride;
+    int T, V;
+    const float *u, *temperature, *top_p, *min_p;    // all but u may be null
+    const int32_t *top_k;
+    int32_t *token;
+    float *logprob, *kept_logprob;                   // may be null
+    void *ws;
+};
+size_t sample_ws_bytes(int T, int V);
+int launch_sample(const SampleArgs &a, hipStream_t s);
 struct AttnArgs {
     KvArgs kv;
     const void *q;

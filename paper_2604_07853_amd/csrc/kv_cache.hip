@@ -17,7 +17,7 @@ __device__ __forceinline__ float head_max(float v)
     return v;
 }
 
-template <int D, bool E4M3>
+template <int D, int FMT>
 __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(KvArgs c, const uint16_t *__restrict__ k, int64_t kts, int64_t khs,
                                                               const uint16_t *__restrict__ v, int64_t vts, int64_t vhs, int64_t T,
                                                               const int64_t *__restrict__ slots)
@@ -38,13 +38,24 @@ __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(KvArgs c, const ui
     const int64_t to = ((page * c.kv_heads + h) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));   // row of the cache
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        if (E4M3) {
+        if (FMT == QARL_KV_E4M3) {
             float f[8];
             bf16x8_to_f32(kv[w], f);
             const LaneScale sc(head_max<D>(LaneScale::absmax8(f, 0.f)));
             if (!live) continue;
             *(u32x2 *)((uint8_t *)(w ? c.v : c.k) + to * D + chunk * 8) = sc.quantize8(f);
             if (chunk == 0) (w ? c.v_scales : c.k_scales)[to] = sc.stored();
+        } else if (FMT == QARL_KV_E2M1) {
+            constexpr int kGroupLanes = kChunks / 4;        // lanes of a group of D / 4 elements
+            float f[8];
+            bf16x8_to_f32(kv[w], f);
+            float absmax = LaneScale::absmax8(f, 0.f);
+#pragma unroll
+            for (int o = kGroupLanes / 2; o > 0; o >>= 1) absmax = fmaxf(absmax, __shfl_xor(absmax, o, 64));
+            const E2m1Scale sc(absmax);
+            if (!live) continue;
+            *(uint32_t *)((uint8_t *)(w ? c.v : c.k) + to * (D / 2) + chunk * 4) = sc.quantize8(f);
+            if (chunk % kGroupLanes == 0) ((uint8_t *)(w ? c.v_scales : c.k_scales))[to * 4 + chunk / kGroupLanes] = sc.byte;
         } else if (live) {
             *(u32x4 *)((uint16_t *)(w ? c.v : c.k) + to * D + chunk * 8) = kv[w];
         }
@@ -61,14 +72,16 @@ int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, co
     }
     const dim3 grid((unsigned)blocks), block(kKvThreads);
     const uint16_t *kp = (const uint16_t *)k, *vp = (const uint16_t *)v;
-    const bool e4m3 = c.fmt == QARL_KV_E4M3;
+#define QARL_KV_WRITE(D) \
+    if (c.fmt == QARL_KV_E4M3) kv_write_kernel<D, QARL_KV_E4M3><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots); \
+    else if (c.fmt == QARL_KV_E2M1) kv_write_kernel<D, QARL_KV_E2M1><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots); \
+    else kv_write_kernel<D, QARL_KV_BF16><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots)
     if (c.head_dim == 128) {
-        if (e4m3) kv_write_kernel<128, true><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots);
-        else kv_write_kernel<128, false><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots);
+        QARL_KV_WRITE(128);
     } else {
-        if (e4m3) kv_write_kernel<64, true><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots);
-        else kv_write_kernel<64, false><<<grid, block, 0, s>>>(c, kp, kts, khs, vp, vts, vhs, T, slots);
+        QARL_KV_WRITE(64);
     }
+#undef QARL_KV_WRITE
     return check_hip(hipGetLastError(), "kv_write_kernel");
 }
 
@@ -79,7 +92,7 @@ int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, co
 constexpr int kReadRows = 16;
 constexpr int64_t kReadCached = (int64_t)64 << 20;
 
-template <int D, bool E4M3, bool NT>
+template <int D, int FMT, bool NT>
 __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvArgs c, const int32_t *__restrict__ table, int64_t table_stride, int table_width,
                                                              const int32_t *__restrict__ offsets, int S, int64_t total,
                                                              uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out)
@@ -117,7 +130,10 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvArgs c, const int
             const int64_t src = at + ((int64_t)h << c.page_shift);
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-                if (E4M3) {
+                if (FMT == QARL_KV_E2M1) {
+                    const uint32_t q4 = load_as<NT, uint32_t>((const uint8_t *)(w ? c.v : c.k) + src * (D / 2) + chunk * 4);
+                    kv[w] = widen_e2m1x8(q4, e2m1_scale((w ? c.v_bytes() : c.k_bytes())[src * 4 + chunk / (kChunks / 4)]));
+                } else if (FMT == QARL_KV_E4M3) {
                     const u32x2 q8 = load_as<NT, u32x2>((const uint8_t *)(w ? c.v : c.k) + src * D + chunk * 8);
                     const float sc = (w ? c.v_scales : c.k_scales)[src];
                     float f[8];
@@ -146,24 +162,25 @@ int launch_kv_read(const KvArgs &c, const int32_t *table, int64_t table_stride, 
     }
     const dim3 grid((unsigned)blocks), block(kKvThreads);
     uint16_t *ko = (uint16_t *)k_out, *vo = (uint16_t *)v_out;
-    const bool e4m3 = c.fmt == QARL_KV_E4M3, nt = total * c.kv_heads * c.head_dim * (e4m3 ? 6 : 8) > kReadCached;
-#define QARL_KV_READ(D, E4M3, NT) kv_read_kernel<D, E4M3, NT><<<grid, block, 0, s>>>(c, table, table_stride, table_width, offsets, S, total, ko, vo)
-#define QARL_KV_READ_AS(D, E4M3) \
-    if (nt) QARL_KV_READ(D, E4M3, true); \
-    else QARL_KV_READ(D, E4M3, false)
-    if (c.head_dim == 128) {
-        if (e4m3) {
-            QARL_KV_READ_AS(128, true);
-        } else {
-            QARL_KV_READ_AS(128, false);
-        }
-    } else {
-        if (e4m3) {
-            QARL_KV_READ_AS(64, true);
-        } else {
-            QARL_KV_READ_AS(64, false);
-        }
+    const bool nt = total * c.kv_heads * c.head_dim * (c.fmt == QARL_KV_BF16 ? 8 : c.fmt == QARL_KV_E4M3 ? 6 : 5) > kReadCached;
+#define QARL_KV_READ(D, FMT, NT) kv_read_kernel<D, FMT, NT><<<grid, block, 0, s>>>(c, table, table_stride, table_width, offsets, S, total, ko, vo)
+#define QARL_KV_READ_AS(D, FMT) \
+    if (nt) QARL_KV_READ(D, FMT, true); \
+    else QARL_KV_READ(D, FMT, false)
+#define QARL_KV_READ_FROM(D) \
+    if (c.fmt == QARL_KV_E4M3) { \
+        QARL_KV_READ_AS(D, QARL_KV_E4M3); \
+    } else if (c.fmt == QARL_KV_E2M1) { \
+        QARL_KV_READ_AS(D, QARL_KV_E2M1); \
+    } else { \
+        QARL_KV_READ_AS(D, QARL_KV_BF16); \
     }
+    if (c.head_dim == 128) {
+        QARL_KV_READ_FROM(128)
+    } else {
+        QARL_KV_READ_FROM(64)
+    }
+#undef QARL_KV_READ_FROM
 #undef QARL_KV_READ_AS
 #undef QARL_KV_READ
     return check_hip(hipGetLastError(), "kv_read_kernel");

@@ -1,0 +1,65 @@
+// Angles of rotary positions.
+//
+// Pair i of a head turns by p f_i at position p.  The descriptor holds f_i / 2 pi as a 64-bit fraction F_i of a turn, so that the low 64 bits of p F_i are
+// the angle modulo a whole turn: exact for every 64-bit p but for the rounding of F_i (2^-65 turns a position; fp32 products p f_i are off by 0.008 rad at
+// p = 131072).  The nearest quarter turn is taken off, the rest lies within an eighth, |x| <= pi / 4, where the power series of sine and cosine up to x^9
+// and x^10 are within 2e-9.
+#pragma once
+#include "common.hpp"
+
+namespace qarl {
+
+// amplitude (cos, sin) of the angle at position p
+__device__ __forceinline__ float2 rope_turn(uint64_t turns, int64_t p, float amplitude)
+{
+    const uint64_t phase = (uint64_t)p * turns;
+    const uint32_t top = (uint32_t)(phase >> 32), quarter = (top + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(top - (quarter << 30)) * (float)(6.283185307179586 / 4294967296.0), x2 = x * x;
+    float s = 1.f / 362880.f, c = -1.f / 3628800.f;
+    s = fmaf(s, x2, -1.f / 5040.f);
+    s = fmaf(s, x2, 1.f / 120.f);
+    s = fmaf(s, x2, -1.f / 6.f);
+    s = fmaf(s * x2, x, x);
+    c = fmaf(c, x2, 1.f / 40320.f);
+    c = fmaf(c, x2, -1.f / 720.f);
+    c = fmaf(c, x2, 1.f / 24.f);
+    c = fmaf(c, x2, -0.5f);
+    c = fmaf(c, x2, 1.f);
+    const bool odd = quarter & 1u;
+    const float cs = odd ? s : c, sn = odd ? c : s;
+    // quarters 1 and 2 have a negative cosine, 2 and 3 a negative sine
+    return make_float2(((quarter + 1u) & 2u ? -cs : cs) * amplitude, (quarter & 2u ? -sn : sn) * amplitude);
+}
+
+// Sixteen elements of a head as two runs of eight: where they begin, for the c-th sixteen.  A rotated one holds eight pairs, 8 c .. 8 c + 7.
+struct RopeRuns {
+    int at[2];
+    bool turned;
+};
+__device__ __forceinline__ RopeRuns rope_runs(int c, int rot, int layout)
+{
+    const bool turned = 16 * c < rot, half = turned && layout == QARL_ROPE_HALF;
+    return RopeRuns{{half ? 8 * c : 16 * c, half ? rot / 2 + 8 * c : 16 * c + 8}, turned};
+}
+
+// The sixteen values turned: y = (a cos - b sin, b cos + a sin) of each pair (a, b)
+__device__ __forceinline__ void rope_apply(float (&x)[16], const float2 (&t)[8], int layout)
+{
+    if (layout == QARL_ROPE_HALF) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = x[i], b = x[8 + i];
+            x[i] = fmaf(a, t[i].x, -(b * t[i].y));
+            x[8 + i] = fmaf(b, t[i].x, a * t[i].y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = x[2 * i], b = x[2 * i + 1];
+            x[2 * i] = fmaf(a, t[i].x, -(b * t[i].y));
+            x[2 * i + 1] = fmaf(b, t[i].x, a * t[i].y);
+        }
+    }
+}
+
+}  // namespace qarl

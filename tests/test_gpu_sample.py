@@ -1,0 +1,223 @@
+"""Sampling of the next token against sorted sums in 64 bits, through the C ABI."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import rollout_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+F32 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def q():
+    from paper_2604_07853_amd import binding
+    binding.lib()
+    return binding
+
+
+def rows_of(T, V, kind, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn((T, V), generator=g) * {"wide": 2.2, "flat": 0.3, "peaked": 1.0, "tiny": 1e-4}[kind]
+    if kind == "peaked":
+        z[torch.arange(T), torch.randint(0, V, (T,), generator=g)] += 9.0
+    return z.to(dtype)
+
+
+def ask(q, z, u, **ways):
+    T = z.shape[0]
+    dt = dict(temperature=torch.float32, top_k=torch.int32, top_p=torch.float32, min_p=torch.float32)
+    kw = {n: torch.as_tensor(v, dtype=dt[n]).expand(T).contiguous().cuda() for n, v in ways.items()}
+    return q.qarl_sample(z.cuda() if not z.is_cuda else z, torch.as_tensor(u, dtype=torch.float32).expand(T).contiguous().cuda(), want_kept=True, **kw)
+
+
+def check(z, got, u, **ways):
+    """Log-probs: a rounding to fp32 of a value of that size, weights left out of the integer sums (below 2^-44 each: 1e-8 at most of 2^20 of them)."""
+    T = z.shape[0]
+    wide = {n: torch.as_tensor(v).expand(T).tolist() for n, v in ways.items()}
+    us = torch.as_tensor(u, dtype=torch.float32).expand(T).tolist()
+    rows = z.cpu().double().numpy()
+    token, lp, kept = got["token"].tolist(), got["logprob"].tolist(), got["kept_logprob"].tolist()
+    for r in range(T):
+        want = ref.sample(rows[r], us[r], **{n: v[r] for n, v in wide.items()})
+        assert token[r] == want[0], (r, token[r], want)
+        for have, w in ((lp[r], want[1]), (kept[r], want[2])):
+            assert (math.isnan(w) and math.isnan(have)) or abs(have - w) <= abs(w) * 1.01 * F32 + 2e-8, (r, have, w)
+
+
+WAYS = [dict(), dict(temperature=0.6, top_k=20, top_p=0.95), dict(top_p=0.9), dict(temperature=1.3, min_p=0.05), dict(top_k=1), dict(temperature=0.0),
+        dict(temperature=0.7, top_k=300, top_p=0.8, min_p=0.01), dict(top_p=0.0), dict(top_k=5000, top_p=0.999), dict(temperature=0.01, top_p=0.5), dict(min_p=2.0)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ways", WAYS)
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1000, 32003])
+def test_all_ways(q, dtype, ways, V):
+    for i, kind in enumerate(("wide", "flat", "peaked", "tiny")):
+        T = 9
+        z = rows_of(T, V, kind, dtype, V + i)
+        u = torch.rand((T,), generator=torch.Generator().manual_seed(V))
+        u[0], u[1] = 0.0, 1.0 - 2.0 ** -24
+        check(z, ask(q, z, u, **ways), u, **ways)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_vocabularies_and_mixed_rows(q, dtype):
+    for T, V in ((37, 151936), (5, (1 << 20) - 3), (3, 1 << 20)):
+        g = torch.Generator().manual_seed(V)
+        z = rows_of(T, V, "wide", dtype, 3)
+        z[T - 1] = rows_of(1, V, "flat", dtype, 4)[0]
+        ways = dict(temperature=torch.rand((T,), generator=g) + 0.5, top_k=torch.randint(0, 3000, (T,), generator=g) * (torch.rand((T,), generator=g) < 0.5),
+                    top_p=torch.rand((T,), generator=g) * 0.6 + 0.5, min_p=torch.rand((T,), generator=g) * 0.01 * (torch.rand((T,), generator=g) < 0.4))
+        ways["temperature"][1] = 0.0
+        u = torch.rand((T,), generator=g)
+        check(z, ask(q, z, u, **ways), u, **ways)
+
+
+@pytest.mark.parametrize("T", [1, 2, 63, 300, 1500])
+def test_many_rows(q, T):
+    z = rows_of(T, 501, "wide", torch.bfloat16, T)
+    u = torch.rand((T,), generator=torch.Generator().manual_seed(T))
+    check(z, ask(q, z, u, top_p=0.9), u, top_p=0.9)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("value", [0.0, -0.0, 5.0, -1e30, 3.3e38, -3.3895313892515355e38, 1e-30, -300.0, 300.0])
+@pytest.mark.parametrize("V", [8, 1000, 70001])
+def test_equal_logits_stand_by_index(q, dtype, value, V):
+    """All V tokens weigh the same: the borders of the sums are whole numbers of weights, met exactly."""
+    z = torch.full((6, V), value).to(dtype)
+    if V > 8 and value == 0.0:
+        z[:, ::2] = -0.0                                # the same value
+    for j in (0, 1, V // 2, V - 1):
+        u = (j + 0.5) / V if V > 8 else j / V          # eighths are exact: the running sum does not yet exceed u at token j - 1
+        got = ask(q, z, u)
+        assert (got["token"] == j).all(), (j, got["token"])
+        assert ((got["logprob"] + math.log(V)).abs() <= math.log(V) * 2 * F32).all()
+    for kw, n in ((dict(top_k=5), 5), (dict(top_p=0.5), -(-V // 2)), (dict(min_p=1.0), V), (dict(min_p=1.5), 1), (dict(top_k=8, top_p=0.25), 2)):
+        for u, want in ((0.0, 0), (1.0, n - 1), (math.nan, 0), (-3.0, 0), (7.0, n - 1)):
+            got = ask(q, z, u, **kw)
+            assert (got["token"] == want).all(), (kw, u, got["token"])
+            assert ((got["kept_logprob"] + math.log(n)).abs() <= math.log(V) * 2 * F32).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_masked_logits(q, dtype):
+    """-inf and the type's lowest value: in front of, behind and between the others; nearly all of a row, all but one."""
+    low = torch.finfo(dtype).min
+    for V, fill in ((50, -math.inf), (50, low), (151936, -math.inf), (151936, low), (70001, -1e4)):
+        z = rows_of(4, V, "wide", dtype, V)
+        z[0, :-3] = fill
+        z[1, 1:] = fill
+        z[2, ::2] = fill
+        z[3, : V // 2] = fill
+        for kw in WAYS[:8]:
+            for u in (0.0, 0.3, 0.999999):
+                check(z, ask(q, z, u, **kw), u, **kw)
+
+
+def test_values_of_every_size(q):
+    """A few large logits over tiny and subnormal ones, values around zero, far from it, and temperatures that make the one like the other."""
+    g = torch.Generator().manual_seed(1)
+    V = 4001
+    for dtype in (torch.bfloat16, torch.float32):
+        z = torch.stack([torch.randn(V, generator=g) * 2.0 ** e for e in (-140, -60, -9, -3, 0, 5, 9, 60, 120)]).to(dtype)
+        z = torch.cat([z, (z[4:5].float() + 600).to(dtype), (z[4:5].float() - 600).to(dtype), (z[4:5].float() * 2.0 ** torch.randint(-20, 8, (V,), generator=g)).to(dtype)])
+        u = torch.rand((z.shape[0],), generator=g)
+        for t in (1.0, 1e-3, 1e-38, 30.0, 1e30):
+            for kw in (dict(), dict(top_p=0.7), dict(top_k=100, min_p=0.2)):
+                check(z, ask(q, z, u, temperature=t, **kw), u, temperature=t, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_without_a_distribution(q, dtype):
+    for V in (9, 5000):
+        z = rows_of(8, V, "wide", dtype, 2)
+        z[0, 3], z[1, V - 1], z[2] = math.nan, math.inf, -math.inf
+        z[3, 1] = -math.nan
+        t = torch.tensor([1.0, 1.0, 1.0, 1.0, -0.5, math.nan, math.inf, 1.0])
+        got = ask(q, z, 0.4, temperature=t)
+        assert got["token"][:7].tolist() == [-1] * 7 and got["logprob"][:7].isnan().all() and got["kept_logprob"][:7].isnan().all()
+        check(z[7:], {n: v[7:] for n, v in got.items()}, 0.4)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("first,pad", [(0, 0), (1, 2), (3, 61), (7, 8)])
+def test_rows_at_any_address(q, dtype, first, pad):
+    V = 3001
+    wide = torch.full((5, first + V + pad), math.nan, dtype=dtype, device="cuda")
+    z = rows_of(5, V, "wide", dtype, 6)
+    wide[:, first: first + V] = z.cuda()
+    view = wide[:, first: first + V]
+    for u in (0.1, 0.9):
+        check(z, ask(q, view, u, top_p=0.95), u, top_p=0.95)
+    check(z[2:3], ask(q, view[2:3], 0.5), 0.5)
+
+
+def test_frequencies_follow_the_probabilities(q):
+    """Evenly spread random numbers: each token comes as often as its share says, to one in either direction."""
+    z = torch.tensor([0.3, 1.7, -0.4, 1.7, 0.0, 2.1, -3.0], dtype=torch.float32)
+    n = 20000
+    u = (torch.arange(n) + 0.5) / n
+    for kw in (dict(), dict(top_k=4), dict(top_p=0.8, temperature=0.7)):
+        got = ask(q, z.expand(n, 7).contiguous(), u, **kw)
+        count = torch.bincount(got["token"].cpu().long(), minlength=7).double()
+        t = kw.get("temperature", 1.0)
+        order = sorted(range(7), key=lambda i: (-float(z[i]), i))
+        w = np.exp([(float(z[i]) - 2.1) / t for i in order])
+        keep = 4 if "top_k" in kw else 1 + int((np.cumsum(w)[:-1] < 0.8 * w.sum()).sum()) if "top_p" in kw else 7
+        for i, j in enumerate(order):
+            want = n * w[i] / w[:keep].sum() if i < keep else 0.0
+            assert abs(count[j] - want) <= 1.01, (kw, j)
+
+
+def test_no_rows_and_results_that_do_not_change(q):
+    assert ask(q, torch.zeros((0, 10), dtype=torch.bfloat16, device="cuda"), 0.5)["token"].shape == (0,)
+    z = rows_of(200, 40001, "flat", torch.float32, 1).cuda()
+    u = torch.rand((200,), generator=torch.Generator().manual_seed(1))
+    first = ask(q, z, u, top_p=0.9)
+    for _ in range(5):
+        again = ask(q, z, u, top_p=0.9)
+        assert all(torch.equal(first[n], again[n]) for n in first)
+    for lo, hi in ((0, 1), (7, 19), (100, 200)):        # by itself or in a batch
+        part = ask(q, z[lo:hi], u[lo:hi], top_p=0.9)
+        assert all(torch.equal(first[n][lo:hi], part[n]) for n in first)
+
+
+def test_graph_and_other_stream(q):
+    T, V = 6, 151936
+    z, u = rows_of(T, V, "wide", torch.bfloat16, 1).cuda(), torch.rand((T,), device="cuda")
+    k, p = torch.tensor([20, 0, 1, 500, 0, 3], dtype=torch.int32, device="cuda"), torch.full((T,), 0.9, device="cuda")
+    out = dict(token=torch.empty((T,), dtype=torch.int32, device="cuda"), logprob=torch.empty((T,), device="cuda"), kept_logprob=torch.empty((T,), device="cuda"))
+    ws = torch.full((max(16, q.qarl_sample_workspace_bytes(T, V)),), 0x5a, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        q.qarl_sample(z, u, top_k=k, top_p=p, ws=ws, **out)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q.qarl_sample(z, u, top_k=k, top_p=p, ws=ws, **out)
+    for seed in range(3):
+        z.copy_(rows_of(T, V, ("wide", "flat", "peaked")[seed], torch.bfloat16, 20 + seed))
+        u.copy_(torch.rand((T,)))
+        ws.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = q.qarl_sample(z, u, top_k=k, top_p=p, want_kept=True)
+        assert all(torch.equal(out[n], want[n]) for n in out)
+        check(z, out, u, top_k=k.cpu(), top_p=0.9)
+
+
+def test_nothing_is_written_behind_the_workspace(q):
+    for T, V, dtype in ((1, 151936, torch.bfloat16), (70, 5000, torch.bfloat16), (3, 20001, torch.float32)):
+        need = q.qarl_sample_workspace_bytes(T, V)
+        ws = torch.full((need + 65536,), 0x5a, dtype=torch.uint8, device="cuda")
+        z = rows_of(T, V, "wide", dtype, 1)
+        u = torch.rand((T,), generator=torch.Generator().manual_seed(1))
+        got = q.qarl_sample(z.cuda(), u.cuda(), want_kept=True, ws=ws)
+        assert (ws[need:] == 0x5a).all()
+        check(z, got, u)
