@@ -8,8 +8,11 @@
 // Sums decide between tokens, and a sum that is off by one part in 10^7 takes another token in one of a thousand rows of a wide distribution.  Weights
 // are therefore computed in 64 bits and summed as integers, in units of 2^-43: whatever the order of the additions, a row's token is the same.
 //
-// 16-bit logits have few values: 4096 bins hold those of size 2^-8 to 2^8 one by one, so that a count says all of a bin, weights are computed once a value
-// and not once a token, and a place in the order is a bin and a number.  (sample_count.. below.)  Rows with others that matter, and 32-bit logits, take the general way.
+// 16-bit logits have few values: 4096 bins hold those of size 2^-9 to 2^7 one by one, so that a count says all of a bin, weights are computed once a value
+// and not once a token, and a place in the order is a bin and a number.  32-bit logits are put into the same bins by their upper halves: these get weights beside
+// their counts, and the tokens of a bin that a place lies in are gathered and sorted.  Rows whose other values matter take a general way, which asks for nothing.
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace qarl {
@@ -42,9 +45,10 @@ struct Row {
     }
     // f(index, value) of this thread's elements of piece i
     template <typename Fn>
-    __device__ __forceinline__ void piece(int i, Fn f) const
+    __device__ __forceinline__ void piece(int i, Fn f) const { elements(i, base[i], f); }
+    template <typename Fn>
+    __device__ __forceinline__ void elements(int i, u32x4 w, Fn f) const
     {
-        const u32x4 w = base[i];
         const int first = i * kPer - off;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
@@ -55,9 +59,21 @@ struct Row {
     template <typename Fn>
     __device__ __forceinline__ void all(Fn f) const
     {
-        for (int i = threadIdx.x; i < pieces; i += kRowThreads) piece(i, f);
+        constexpr int kAhead = 4;       // pieces requested at once
+        for (int i = threadIdx.x; i < pieces; i += kAhead * kRowThreads) {
+            u32x4 w[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (i + j * kRowThreads < pieces) w[j] = base[i + j * kRowThreads];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (i + j * kRowThreads < pieces) elements(i + j * kRowThreads, w[j], f);
+        }
     }
 };
+
+// (2^52 added: the sum's last bit is a unit)
+__device__ __forceinline__ unsigned long long weight_units(double w) { return (unsigned long long)__double_as_longlong(w * kUnit + 4503599627370496.0) & 0xfffffffffffffull; }
 
 // e^y for y <= 0 in units of 2^-43, rounded to nearest even; `w`: e^y itself.  y = k ln 2 + r, |r| <= ln 2 / 2: the power series of e^r up to r^12 is within 1e-16
 __device__ __forceinline__ unsigned long long weight_of(double y, double &w)
@@ -82,8 +98,7 @@ __device__ __forceinline__ unsigned long long weight_of(double y, double &w)
     p = fma(p, r, 1.0);
     p = fma(p, r, 1.0);
     w = ldexp(p, (int)k);
-    // (2^52 added: the sum's last bit is a unit)
-    return (unsigned long long)__double_as_longlong(w * kUnit + 4503599627370496.0) & 0xfffffffffffffull;
+    return weight_units(w);
 }
 
 struct Bins {
@@ -273,9 +288,9 @@ __device__ __forceinline__ void no_token(const SampleArgs &a, int r)
     if (a.kept_logprob) a.kept_logprob[r] = __builtin_nanf("");
 }
 
-__device__ __forceinline__ void give(const SampleArgs &a, int r, int token, double y, unsigned long long whole, unsigned long long kept)
+// y: the token's logit less the largest, over t
+__device__ __forceinline__ void log_probs(const SampleArgs &a, int r, double y, unsigned long long whole, unsigned long long kept)
 {
-    a.token[r] = token;
     if (a.logprob) a.logprob[r] = (float)(y - log((double)whole / kUnit));
     if (a.kept_logprob) a.kept_logprob[r] = (float)(y - log((double)kept / kUnit));
 }
@@ -349,7 +364,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, int r, RowLds &s
     if (ask.k > 0 && (uint32_t)ask.k < n) first_tokens((uint32_t)ask.k);
     if (ask.top_p < 1.f && n > 1) {
         const double goal = (double)fmaxf(ask.top_p, 0.f) * (double)kept;
-        const Place p = x.find([goal](uint32_t, unsigned long long w) { return (double)w >= goal; });
+        const unsigned long long least = (unsigned long long)ceil(goal);
+        const Place p = x.find([least](uint32_t, unsigned long long w) { return w >= least; });
         if (p.there) {
             const double more = p.each ? ceil((goal - (double)p.mass) / (double)p.each) : 1.0;
             const uint32_t in = (uint32_t)fmin(fmax(more, 1.0), (double)p.equal);
@@ -361,8 +377,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, int r, RowLds &s
     }
     if (n_min < n) first_tokens(n_min);
     // ---- the token
-    const double goal = (ask.u >= 0.f ? (double)ask.u : 0.0) * (double)kept;
-    Place p = x.find([goal](uint32_t, unsigned long long w) { return (double)w > goal; });
+    const double goal = (ask.u >= 0.f ? fmin((double)ask.u, 1.0) : 0.0) * (double)kept;
+    const unsigned long long below = (unsigned long long)goal;
+    Place p = x.find([below](uint32_t, unsigned long long w) { return w > below; });
     uint32_t nth = 0;
     if (p.there && p.before < n) {
         nth = p.each ? (uint32_t)fmin(fmax(floor((goal - (double)p.mass) / (double)p.each), 0.0), (double)(p.equal - 1)) : 0u;
@@ -408,42 +425,34 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, int r, RowLds &s
                 ++seen;
             }
         });
-        give(a, r, token, ((double)key_value(p.key) - (double)x.m) * x.inv_t, whole, kept);
+        a.token[r] = token;
+        log_probs(a, r, ((double)key_value(p.key) - (double)x.m) * x.inv_t, whole, kept);
     }
-}
-
-template <bool F32>
-__global__ __launch_bounds__(kRowThreads) void sample_rows_kernel(SampleArgs a)
-{
-    extern __shared__ __align__(16) char lds[];
-    sample_row<F32>(a, blockIdx.x, *(RowLds *)lds);
 }
 
 // ---- 16-bit logits by value.  A pattern less kFirst, of which bits 11 to 14 are then zero, names its bin: bit 15 the sign, bits 0 to 10 the size.
 constexpr uint32_t kFirst = 118 << 7;       // 2^-9
 constexpr double kLowest = 128.0;           // 2^7: sixteen powers of two on
 constexpr int kSide = 2048;                 // bins of a sign
-constexpr int kRare = 2048;                 // room for values below 2^-9 other than zero (one of 1400 tokens of logits that spread by 2.2)
+constexpr int kRare = 1024;                 // room for values of a sign below 2^-9 other than zero (one of 2800 tokens of logits that spread by 2.2)
 constexpr uint32_t kNone = 0xff80ff80u;     // two -inf
-constexpr int kMostParts = 32;
-
-// Where the bins' counts come from: a workgroup that takes a row by itself counts its quarters apart, two to a word; or parts of a row were counted by workgroups
-// of their own.  (The part that a token lies in is searched for it; the others need not be read again.)
-struct PartCounts {             // in the workspace, for each part
-    uint16_t count[2 * kSide];  // by size, the signs side by side: a part has at most 65535 tokens
-    uint32_t zeros, flags, rare, unused;
-    uint2 list[kRare / 4];      // index, pattern
-};
+constexpr int kMostParts = 32, kPartRare = 256, kRuns = 8;
 enum { kBad = 1, kHigh = 2, kLow = 4 };
 
+// What the workgroup that counts a part of a row leaves of it
+struct PartCounts {
+    uint16_t count[2 * kSide];  // by size, the signs side by side: a part has at most 65535 tokens
+    uint32_t zeros, flags, rare[2];
+    unsigned long long list[2][kPartRare];  // key and index of the rare values, by sign
+};
+
 struct ChooseLds {
-    uint32_t bins[2][2 * kSide];
-    unsigned long long list[kRare];         // the rare values: what they are sorted by (choose), before that their index and pattern
+    uint32_t bins[2][2 * kSide];            // a row's quarters, two to a word (row by row); the first half: a part's counts
+    unsigned long long list[3][kRare];      // the rare values by sign: key and index; 32-bit logits: those of one bin
     unsigned long long wave_mass[kRowWaves], rare_mass[2], rare_sum[kRowWaves];
-    uint32_t wave_count[kRowWaves], wave_first[kRowWaves];
-    uint32_t rare_count[2], rare_top[2];
-    uint32_t rare, zeros, flags, n_min, sorted;
-    uint32_t runs[64], part_at[kMostParts + 1];
+    uint32_t wave_count[kRowWaves], wave_first[kRowWaves], wave_hit[2][kRowWaves];
+    uint32_t rare[2], sorted[2], flags, n_min, top, zeros[kMostParts], gathered, in_bin, bin_sorted;
+    uint32_t runs[kRuns];
     Place place[2][kRowWaves], spot;
     uint32_t owner;
 };
@@ -451,264 +460,335 @@ union ValueLds {
     ChooseLds choose;
     RowLds row;         // for rows that take the general way
 };
+struct FloatLds : ChooseLds {
+    unsigned long long mass[2 * kSide];
+};
+union WideLds {
+    FloatLds choose;
+    RowLds row;
+};
 
 __device__ __forceinline__ float pattern_value(uint32_t b) { return __uint_as_float(b << 16); }
-// place of the bin number `bin` of the order among the counts: sizes rising, the signs side by side
-__device__ __forceinline__ int bin_slot(int bin) { return bin < kSide ? 2 * (kSide - 1 - bin) : 2 * (bin - kSide) + 1; }
 __device__ __forceinline__ uint32_t bin_pattern(int bin) { return bin < kSide ? kFirst + (uint32_t)(kSide - 1 - bin) : 0x8000u + kFirst + (uint32_t)(bin - kSide); }
 
-// Two values into the bins (`bump` to be added to their counts), or to what is kept of others
-__device__ __forceinline__ void count_pair(uint32_t w, int index, uint32_t *bins, uint32_t bump, ChooseLds &s, uint32_t &zeros, uint32_t &flags)
+// Inclusive sums over a wavefront, or over each 16 lanes of it: row shifts and two row broadcasts
+#define QARL_SCAN_STEP(CTRL, ROWS) \
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false)
+#define QARL_SCAN_STEP64(CTRL, ROWS) \
+    v += (unsigned long long)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false) << 32 | \
+         (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false)
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t v)
 {
-    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
-    const u16x2 r = __builtin_bit_cast(u16x2, w) - (u16x2){(uint16_t)kFirst, (uint16_t)kFirst};
-    const uint32_t slot = __builtin_bit_cast(uint32_t, (u16x2)(r << 1)) | __builtin_bit_cast(uint32_t, (u16x2)(r >> 15));
-    const uint32_t rw = __builtin_bit_cast(uint32_t, r);
-    if ((rw & 0x78007800u) == 0) {
-        atomicAdd((uint32_t *)((char *)bins + ((slot << 2) & 0x3fffcu)), bump);
-        atomicAdd((uint32_t *)((char *)bins + ((slot >> 14) & 0x3fffcu)), bump);
-        return;
+    QARL_SCAN_STEP(0x111, 0xf);
+    QARL_SCAN_STEP(0x112, 0xf);
+    QARL_SCAN_STEP(0x114, 0xf);
+    QARL_SCAN_STEP(0x118, 0xf);
+    if (WHOLE) {
+        QARL_SCAN_STEP(0x142, 0xa);
+        QARL_SCAN_STEP(0x143, 0xc);
     }
-    if (w == kNone) return;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const uint32_t b = e ? w >> 16 : w & 0xffffu, rb = e ? rw >> 16 : rw & 0xffffu, size = b & 0x7fffu;
-        if ((rb & 0x7800u) == 0) {
-            atomicAdd(bins + (e ? slot >> 16 : slot & 0xffffu), bump);
-        } else if (size == 0) {
-            ++zeros;
-        } else if (size < kFirst) {
-            const uint32_t at = atomicAdd(&s.rare, 1u);
-            if (at < (uint32_t)kRare) s.list[at] = (unsigned long long)b << 32 | (uint32_t)(index + e);
-        } else if (b != 0xff80u) {
-            flags |= size >= 0x7f80u ? kBad : b & 0x8000u ? kLow : kHigh;
-        }
-    }
+    return v;
 }
-// Eight values; those outside the row become -inf
-__device__ __forceinline__ void count_piece(u32x4 w, int first, int V, uint32_t *bins, uint32_t bump, ChooseLds &s, uint32_t &zeros, uint32_t &flags)
+template <bool WHOLE>
+__device__ __forceinline__ unsigned long long scan_lanes(unsigned long long v)
 {
-    if (first < 0 || first + 8 > V) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if ((unsigned)(first + e) >= (unsigned)V) w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | (kNone & 0xffff0000u) : (w[e >> 1] & 0xffff0000u) | (kNone & 0xffffu);
+    QARL_SCAN_STEP64(0x111, 0xf);
+    QARL_SCAN_STEP64(0x112, 0xf);
+    QARL_SCAN_STEP64(0x114, 0xf);
+    QARL_SCAN_STEP64(0x118, 0xf);
+    if (WHOLE) {
+        QARL_SCAN_STEP64(0x142, 0xa);
+        QARL_SCAN_STEP64(0x143, 0xc);
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) count_pair(w[e], first + 2 * e, bins, bump, s, zeros, flags);
+    return v;
+}
+#undef QARL_SCAN_STEP
+#undef QARL_SCAN_STEP64
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ unsigned long long lane_of(unsigned long long v, int lane)
+{
+    return (unsigned long long)lane_of((uint32_t)(v >> 32), lane) << 32 | lane_of((uint32_t)v, lane);
 }
 
+// Two values into the bins (`bump` to be added to their counts), or to what is kept of others
+struct Counts {
+    uint32_t *bins, *rare;
+    unsigned long long *list;
+    uint32_t room, zeros, flags;
+    __device__ __forceinline__ void pair(uint32_t w, int index, uint32_t bump)
+    {
+        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+        const u16x2 r = __builtin_bit_cast(u16x2, w) - (u16x2){(uint16_t)kFirst, (uint16_t)kFirst};
+        const uint32_t slot = __builtin_bit_cast(uint32_t, (u16x2)(r << 1)) | __builtin_bit_cast(uint32_t, (u16x2)(r >> 15));
+        const uint32_t rw = __builtin_bit_cast(uint32_t, r);
+        if ((rw & 0x78007800u) == 0) {
+            atomicAdd((uint32_t *)((char *)bins + ((slot << 2) & 0x3fffcu)), bump);
+            atomicAdd((uint32_t *)((char *)bins + ((slot >> 14) & 0x3fffcu)), bump);
+            return;
+        }
+        if (w == kNone) return;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t b = e ? w >> 16 : w & 0xffffu, rb = e ? rw >> 16 : rw & 0xffffu, size = b & 0x7fffu;
+            if ((rb & 0x7800u) == 0) {
+                atomicAdd(bins + (e ? slot >> 16 : slot & 0xffffu), bump);
+            } else if (size == 0) {
+                ++zeros;
+            } else if (size < kFirst) {
+                const uint32_t at = atomicAdd(rare + (b >> 15), 1u);
+                if (at < room) list[(b >> 15) * room + at] = (unsigned long long)order_key(pattern_value(b)) << 32 | (uint32_t)(index + e);
+            } else if (b != 0xff80u) {
+                flags |= size >= 0x7f80u ? kBad : b & 0x8000u ? kLow : kHigh;
+            }
+        }
+    }
+    // Eight values; those outside the row become -inf
+    __device__ __forceinline__ void piece(u32x4 w, int first, int V, uint32_t bump)
+    {
+        if (first < 0 || first + 8 > V) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((unsigned)(first + e) >= (unsigned)V) w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | (kNone & 0xffff0000u) : (w[e >> 1] & 0xffff0000u) | (kNone & 0xffffu);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pair(w[e], first + 2 * e, bump);
+    }
+};
+
 struct Chosen {
-    uint32_t pattern;       // the token's value
-    uint32_t nth;           // of the tokens with that value; of a rare one: its index
-    bool rare, none;
-    double y;
-    unsigned long long whole, kept;
+    uint32_t key;           // the token's value
+    uint32_t nth;           // of the tokens with that value; of one out of a list: its index
+    bool listed, none;
 };
 
 // What the counts of a row say.  Thread i holds bins 4 i .. 4 i + 3 of the order: positive values falling, then negative ones; the rare ones and zero stand between.
+template <bool F32>
 struct Chooser {
+    using Lds = typename std::conditional<F32, FloatLds, ChooseLds>::type;
     static constexpr int kEach = 2 * kSide / kRowThreads;
-    ChooseLds &s;
-    uint32_t c[kEach], cb;
-    unsigned long long unit[kEach], mb;
-    uint32_t special[3];                        // tokens of the rare positive values, of zero, of the rare negative ones
-    unsigned long long special_mass[3], zero_unit;
+    Lds &s;
+    const Row<F32> &row;
+    uint32_t c[kEach], upto[kEach];                 // tokens of the bins, and of the order up to their ends
+    unsigned long long unit[kEach], mass[kEach];    // a token's weight (32-bit logits: the bin's), and that of the order up to the bins' ends
+    uint32_t positive, special[3];              // tokens of the positive bins; of the rare positive values, of zero, of the rare negative ones
+    unsigned long long positive_mass, special_mass[3], zero_unit;
     float m;
     double inv_t;
     int calls;
+    bool lost;                                  // 32-bit logits: a bin's tokens are more than there is room for
 
     __device__ __forceinline__ unsigned long long weigh(float z, double &w) const { return weight_of(((double)z - (double)m) * inv_t, w); }
 
-    // The place among the rare values of a sign, each a bin of its own.  They are sorted the first time that one is asked for: by value falling, then index.
-    // (`from`, `count`: of that sign; the result in s.spot, its index in s.owner.  A function of its own: it is seldom called, and costs the others registers.)
+    // The place among the n <= kRowThreads tokens of a list of keys and indices, each a bin of its own: sorted the first time that one is asked for.
+    // (The result in s.spot, its index in s.owner.  A function of its own: it is seldom called, and costs the others registers.)
     template <typename Fn>
-    __device__ static __attribute__((noinline)) void among_rare(ChooseLds &s, uint32_t from, uint32_t count, uint32_t before, unsigned long long mass, float m, double inv_t, Fn pass)
+    __device__ static __attribute__((noinline)) void among(ChooseLds &s, unsigned long long *list, uint32_t n, uint32_t *sorted, uint32_t before, unsigned long long mass, float m,
+                                                           double inv_t, Fn pass)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const uint32_t n = s.rare;
         __syncthreads();
-        if (!s.sorted) {
+        if (!*sorted) {
             uint32_t size = 2;
             while (size < n) size *= 2;
-            for (uint32_t i = threadIdx.x; i < size; i += kRowThreads) {
-                unsigned long long k = ~0ull;
-                if (i < n) {
-                    const uint32_t b = (uint32_t)(s.list[i] >> 32);     // (patterns of positive values turned round: falling)
-                    k = (unsigned long long)(b >> 15 ? b : 0x7fffu - b) << 32 | (uint32_t)s.list[i];
-                }
-                s.list[i] = k;
-            }
+            if (threadIdx.x >= n && threadIdx.x < size) list[threadIdx.x] = ~0ull;
             for (uint32_t k = 2; k <= size; k *= 2) {
                 for (uint32_t j = k / 2; j > 0; j /= 2) {
                     __syncthreads();
-                    for (uint32_t t = threadIdx.x; t < size / 2; t += kRowThreads) {
-                        const uint32_t a = 2 * t - (t & (j - 1)), b = a + j;
-                        const unsigned long long x = s.list[a], y = s.list[b];
+                    if (threadIdx.x < size / 2) {
+                        const uint32_t t = threadIdx.x, a = 2 * t - (t & (j - 1)), b = a + j;
+                        const unsigned long long x = list[a], y = list[b];
                         if ((x > y) == ((a & k) == 0)) {
-                            s.list[a] = y;
-                            s.list[b] = x;
+                            list[a] = y;
+                            list[b] = x;
                         }
                     }
                 }
             }
             __syncthreads();
-            if (threadIdx.x == 0) s.sorted = 1;
+            if (threadIdx.x == 0) *sorted = 1;
         }
-        // positive ones stand in front; thread i takes entries 2 i and 2 i + 1 of its sign
-        unsigned long long u[2] = {0, 0}, key[2] = {0, 0};
-        double w;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t i = 2 * threadIdx.x + e;
-            if (i < count) {
-                key[e] = s.list[from + i];
-                const uint32_t b = (uint32_t)(key[e] >> 32);
-                key[e] = (unsigned long long)(b >> 15 ? b : 0x7fffu - b) << 32 | (uint32_t)key[e];
-                u[e] = weight_of(((double)pattern_value((uint32_t)(key[e] >> 32)) - (double)m) * inv_t, w);
-            }
+        uint32_t key = 0, index = 0;
+        unsigned long long u = 0;
+        if (threadIdx.x < n) {
+            index = (uint32_t)list[threadIdx.x];
+            key = (uint32_t)(list[threadIdx.x] >> 32);
+            double w;
+            u = weight_of(((double)key_value(key) - (double)m) * inv_t, w);
         }
-        unsigned long long wi = u[0] + u[1];
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const unsigned long long up = __shfl_up(wi, o, 64);
-            if (lane >= o) wi += up;
-        }
-        if (lane == 63) s.rare_sum[wave] = wi;
+        const unsigned long long upto = scan_lanes<true>(u);
+        if (lane == 63) s.rare_sum[wave] = upto;
         __syncthreads();
-        mass += wi - u[0] - u[1];
+        mass += upto - u;
         for (int i = 0; i < wave; ++i) mass += s.rare_sum[i];
-        before += 2 * threadIdx.x;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t i = 2 * threadIdx.x + e;
-            // the first that passes: what stands in front of it does not
-            if (i < count && pass(before + 1, mass + u[e]) && (i == 0 || !pass(before, mass))) {
-                s.spot = Place{(uint32_t)(key[e] >> 32), before, 1, mass, u[e], true};
-                s.owner = (uint32_t)key[e];
-            }
-            before += 1;
-            mass += u[e];
+        before += threadIdx.x;
+        // the first that passes: what stands in front of it does not
+        if (threadIdx.x < n && pass(before + 1, mass + u) && (threadIdx.x == 0 || !pass(before, mass))) {
+            s.spot = Place{key, before, 1, mass, u, true};
+            s.owner = index;
         }
+        __syncthreads();
+    }
+
+    // 32-bit logits: the tokens of a bin into the third list
+    __device__ __forceinline__ void gather(uint32_t pattern)
+    {
+        __syncthreads();
+        if (s.gathered == pattern) return;      // (they are there)
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            s.gathered = pattern;
+            s.in_bin = 0;
+            s.bin_sorted = 0;
+        }
+        __syncthreads();
+        row.all([&](int index, float z) {
+            if (__float_as_uint(z) >> 16 == pattern) {
+                const uint32_t at = atomicAdd(&s.in_bin, 1u);
+                if (at < (uint32_t)kRare) s.list[2][at] = (unsigned long long)order_key(z) << 32 | (uint32_t)index;
+            }
+        });
         __syncthreads();
     }
 
     template <typename Fn>
-    __device__ __forceinline__ Place find(Fn pass, bool &rare)
+    __device__ __forceinline__ Place find(Fn pass, bool &listed)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        Place *const places = s.place[calls++ & 1];     // (the other half may still be read)
-        Place mine = {};
-        uint32_t before = cb;
-        unsigned long long mass = mb;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            if (!mine.there && c[i] && pass(before + c[i], mass + c[i] * unit[i])) mine = Place{bin_pattern(threadIdx.x * kEach + i), before, c[i], mass, unit[i], true};
-            before += c[i];
-            mass += c[i] * unit[i];
-        }
-        const unsigned long long hit = __ballot(mine.there);
-        if (lane == (hit ? __ffsll((long long)hit) - 1 : 0)) places[wave] = mine;
-        __syncthreads();
-        rare = false;
-#pragma unroll 1
-        for (int i = 0; i < kRowWaves; ++i) {
-            if (i == kRowWaves / 2) {       // between the signs
-                uint32_t b = 0;
-                unsigned long long w = 0;
-                for (int j = 0; j < kRowWaves / 2; ++j) {
-                    b += s.wave_count[j];
-                    w += s.wave_mass[j];
-                }
-                for (int j = 0; j < 3; ++j) {
-                    if (special[j] && pass(b + special[j], w + special_mass[j])) {
-                        if (j == 1) return Place{0, b, special[1], w, zero_unit, true};
-                        rare = true;
-                        among_rare(s, j ? special[0] : 0, special[j], b, w, m, inv_t, pass);
-                        return s.spot;
-                    }
-                    b += special[j];
-                    w += special_mass[j];
-                }
-            }
-            if (places[i].there) return places[i];
-        }
-        return Place{};
-    }
-
-    // False where the row has to take the general way
-    __device__ __forceinline__ bool choose(const RowAsk &ask, Chosen &out)
-    {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        calls = 0;
-        const uint32_t n_rare = min(s.rare, (uint32_t)kRare);
-        // ---- the largest value
-        int first = -1;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = calls++ & 1;     // (what the call before has found may still be read)
+        bool hit_here = false;
+        Place mine;
 #pragma unroll
         for (int i = kEach - 1; i >= 0; --i)
-            if (c[i]) first = threadIdx.x * kEach + i;
-        const unsigned long long some = __ballot(first >= 0);
-        if (lane == (some ? __ffsll((long long)some) - 1 : 0)) s.wave_first[wave] = (uint32_t)first;
-        for (uint32_t i = threadIdx.x; i < n_rare; i += kRowThreads) {
-            const uint32_t b = (uint32_t)(s.list[i] >> 32);
-            if (b >> 15) atomicMin(&s.rare_top[1], b);
-            else atomicMax(&s.rare_top[0], b);
-            atomicAdd(&s.rare_count[b >> 15], 1u);
+            if (c[i] && pass(upto[i], mass[i])) {
+                hit_here = true;
+                mine = Place{bin_pattern(threadIdx.x * kEach + i), upto[i], c[i], mass[i], unit[i], true};
+            }
+        const unsigned long long hit = __ballot(hit_here);
+        if (lane == 0) s.wave_hit[half][wave] = hit != 0;
+        if (hit && lane == __ffsll((long long)hit) - 1) {
+            mine.before -= mine.equal;
+            mine.mass -= F32 ? mine.each : mine.equal * mine.each;
+            s.place[half][wave] = mine;
         }
         __syncthreads();
-        out.none = true;
-        if ((s.flags & kBad) || !usable(ask.t)) return true;
-        if ((s.flags & kHigh) || s.rare > (uint32_t)kRare) return false;
-        special[0] = s.rare_count[0];
-        special[1] = s.zeros;
-        special[2] = s.rare_count[1];
-        uint32_t top = 0xffffffffu;
-        for (int i = 0; i < kRowWaves && top == 0xffffffffu; ++i) {
-            if (i == kRowWaves / 2) {
-                if (special[0]) top = s.rare_top[0];
-                else if (special[1]) top = 0;
-                else if (special[2]) top = s.rare_top[1];
-                if (top != 0xffffffffu) break;
+        const uint32_t hits = (uint32_t)__ballot(lane < kRowWaves && s.wave_hit[half][lane & (kRowWaves - 1)] != 0);
+        listed = false;
+        if (!(hits & 0xffu)) {
+            uint32_t b = positive;          // between the signs
+            unsigned long long w = positive_mass;
+#pragma unroll
+            for (int j = 0; j < 3; ++j) {
+                if (special[j] && pass(b + special[j], w + special_mass[j])) {
+                    if (j == 1) return Place{order_key(0.f), b, special[1], w, zero_unit, true};
+                    listed = true;
+                    among(s, s.list[j >> 1], special[j], &s.sorted[j >> 1], b, w, m, inv_t, pass);
+                    return s.spot;
+                }
+                b += special[j];
+                w += special_mass[j];
             }
-            if ((int)s.wave_first[i] >= 0) top = bin_pattern((int)s.wave_first[i]);
+            if (!hits) return Place{};
         }
-        if (top == 0xffffffffu) return !(s.flags & kLow);       // (only -inf: no token)
-        m = pattern_value(top);
-        inv_t = 1.0 / (double)ask.t;
-        if ((s.flags & kLow) && ((double)m + kLowest) * inv_t < 31.0) return false;     // those of -128 and less weigh a unit or more
-        // ---- weights
-        uint32_t csum = 0, above = 0;
+        Place p = s.place[half][__ffs((int)hits) - 1];
+        if (F32) {
+            gather(p.key);
+            const uint32_t n = s.in_bin;
+            if (n > (uint32_t)kRare) {
+                lost = true;
+                return p;
+            }
+            listed = true;
+            among(s, s.list[2], n, &s.bin_sorted, p.before, p.mass, m, inv_t, pass);
+            return s.spot;
+        }
+        p.key = order_key(pattern_value(p.key));
+        return p;
+    }
+
+    // False where the row has to take the general way.  Writes the log-probs.  32-bit logits: the largest one's key is s.top, the bins' weights are s.mass.
+    __device__ __forceinline__ bool choose(const SampleArgs &a, int r, const RowAsk &ask, uint32_t zeros, Chosen &out)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & (kRowWaves - 1);
+        calls = 0;
+        lost = false;
+        const uint32_t n_rare[2] = {min(s.rare[0], (uint32_t)kRare), min(s.rare[1], (uint32_t)kRare)};
+        double w = 0.0;
+        uint32_t csum = 0;
         unsigned long long wsum = 0;
-        double w;
+        out.none = true;
+        if (!F32) {
+            // ---- the largest value
+            int first = kEach;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            unit[i] = 0;
-            if (c[i]) {
-                unit[i] = weigh(pattern_value(bin_pattern(threadIdx.x * kEach + i)), w);
-                if (w >= (double)ask.min_p) above += c[i];
+            for (int i = kEach - 1; i >= 0; --i)
+                if (c[i]) first = i;
+            const unsigned long long some = __ballot(first < kEach);
+            if (lane == (some ? __ffsll((long long)some) - 1 : 0)) s.wave_first[wave] = some ? threadIdx.x * kEach + first : 0xffffffffu;
+            __syncthreads();
+            if ((s.flags & kBad) || !usable(ask.t)) return true;
+            if ((s.flags & kHigh) || s.rare[0] > (uint32_t)kRare || s.rare[1] > (uint32_t)kRare) return false;
+            const uint32_t tops = s.wave_first[l16], with = (uint32_t)__ballot(lane < kRowWaves && tops != 0xffffffffu);
+            if (with & 0xffu) m = pattern_value(bin_pattern((int)lane_of(tops, __ffs((int)with) - 1)));
+            else if (n_rare[0] || (!zeros && n_rare[1])) {      // a rare one
+                const int sign = !n_rare[0];
+                if (threadIdx.x < n_rare[sign]) atomicMin(&s.top, (uint32_t)(s.list[sign][threadIdx.x] >> 32));
+                __syncthreads();
+                m = key_value(s.top);
+            } else if (zeros) m = 0.f;
+            else if (with) m = pattern_value(bin_pattern((int)lane_of(tops, __ffs((int)with) - 1)));
+            else return !(s.flags & kLow);      // (only -inf: no token)
+            inv_t = 1.0 / (double)ask.t;
+            if ((s.flags & kLow) && ((double)m + kLowest) * inv_t < 31.0) return false;     // those of -128 and less weigh a unit or more
+            // ---- weights.  A thread's values lie a step apart: the first one's weight by the exponential, the others by a factor
+            uint32_t above = 0;
+            double factor = 0.0;
+            if (first < kEach) {
+                const uint32_t b = bin_pattern(threadIdx.x * kEach + first);
+                const float z = pattern_value(b), next = pattern_value(b + (b >> 15 ? 1 : -1));
+                weigh(z, w);
+                weight_of(((double)next - (double)z) * inv_t, factor);
             }
-            csum += c[i];
-            wsum += c[i] * unit[i];
-        }
-        for (uint32_t i = threadIdx.x; i < n_rare; i += kRowThreads) {
-            const uint32_t b = (uint32_t)(s.list[i] >> 32);
-            const unsigned long long units = weigh(pattern_value(b), w);
-            if (units) atomicAdd(&s.rare_mass[b >> 15], units);
-            above += w >= (double)ask.min_p;
-        }
-        zero_unit = weigh(0.f, w);
-        if (threadIdx.x == 0 && w >= (double)ask.min_p) above += special[1];
-        if (ask.min_p > 0.f && above) atomicAdd(&s.n_min, above);
-        uint32_t ci = csum;
-        unsigned long long wi = wsum;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t cu = __shfl_up(ci, o, 64);
-            const unsigned long long wu = __shfl_up(wi, o, 64);
-            if (lane >= o) {
-                ci += cu;
-                wi += wu;
+            for (int i = 0; i < kEach; ++i) {
+                if (i > first) w *= factor;
+                unit[i] = c[i] ? weight_units(w) : 0;
+                above += w >= (double)ask.min_p ? c[i] : 0;
+                csum += c[i];
+                wsum += c[i] * unit[i];
             }
+#pragma unroll
+            for (int sign = 0; sign < 2; ++sign) {
+                if ((uint32_t)(wave * 64) < n_rare[sign]) {
+                    unsigned long long units = 0;
+                    if (threadIdx.x < n_rare[sign]) {
+                        units = weigh(key_value((uint32_t)(s.list[sign][threadIdx.x] >> 32)), w);
+                        above += w >= (double)ask.min_p;
+                    }
+                    units = scan_lanes<true>(units);
+                    if (lane == 63) atomicAdd(&s.rare_mass[sign], units);
+                }
+            }
+            zero_unit = 0;
+            if (zeros) {
+                zero_unit = weigh(0.f, w);
+                if (threadIdx.x == 0 && w >= (double)ask.min_p) above += zeros;
+            }
+            if (ask.min_p > 0.f && above) atomicAdd(&s.n_min, above);
+        } else {
+            if ((s.flags & kHigh) || s.rare[0] > (uint32_t)kRare || s.rare[1] > (uint32_t)kRare) return false;
+            if ((s.flags & kLow) && ((double)m + kLowest) * inv_t < 31.0) return false;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                csum += c[i];
+                wsum += unit[i];
+            }
+            zero_unit = zeros ? weigh(0.f, w) : 0;
         }
+        special[0] = n_rare[0];
+        special[1] = zeros;
+        special[2] = n_rare[1];
+        const uint32_t ci = scan_lanes<true>(csum);
+        const unsigned long long wi = scan_lanes<true>(wsum);
         if (lane == 63) {
             s.wave_count[wave] = ci;
             s.wave_mass[wave] = wi;
@@ -717,35 +797,37 @@ struct Chooser {
         special_mass[0] = s.rare_mass[0];
         special_mass[1] = special[1] * zero_unit;
         special_mass[2] = s.rare_mass[1];
-        cb = ci - csum;
-        mb = wi - wsum;
+        const uint32_t wc = s.wave_count[l16], wcs = scan_lanes<false>(wc);
+        const unsigned long long wm = s.wave_mass[l16], wms = scan_lanes<false>(wm);
+        positive = lane_of(wcs, kRowWaves / 2 - 1);
+        positive_mass = lane_of(wms, kRowWaves / 2 - 1);
         uint32_t n = special[0] + special[1] + special[2];
         unsigned long long whole = special_mass[0] + special_mass[1] + special_mass[2];
-        if (wave >= kRowWaves / 2) {
-            cb += n;
-            mb += whole;
+        const int at = __builtin_amdgcn_readfirstlane(wave);
+        uint32_t cb = ci - csum + lane_of(wcs, at) - lane_of(wc, at) + (at >= kRowWaves / 2 ? n : 0);
+        unsigned long long mb = wi - wsum + lane_of(wms, at) - lane_of(wm, at) + (at >= kRowWaves / 2 ? whole : 0);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            upto[i] = cb += c[i];
+            mass[i] = mb += F32 ? unit[i] : c[i] * unit[i];
         }
-#pragma unroll 1
-        for (int i = 0; i < kRowWaves; ++i) {
-            if (i < wave) {
-                cb += s.wave_count[i];
-                mb += s.wave_mass[i];
-            }
-            n += s.wave_count[i];
-            whole += s.wave_mass[i];
-        }
+        n += lane_of(wcs, kRowWaves - 1);
+        whole += lane_of(wms, kRowWaves - 1);
         // ---- what is kept, and the token
         unsigned long long kept = whole;
-        bool rare;
+        bool listed;
         const auto first_tokens = [&](uint32_t k) {
-            const Place p = find([k](uint32_t x, unsigned long long) { return x >= k; }, rare);
+            const Place p = find([k](uint32_t x, unsigned long long) { return x >= k; }, listed);
             n = k;
             kept = p.mass + (k - p.before) * p.each;
         };
         if (ask.k > 0 && (uint32_t)ask.k < n) first_tokens((uint32_t)ask.k);
+        if (F32 && lost) return false;
         if (ask.top_p < 1.f && n > 1) {
             const double goal = (double)fmaxf(ask.top_p, 0.f) * (double)kept;
-            const Place p = find([goal](uint32_t, unsigned long long x) { return (double)x >= goal; }, rare);
+            const unsigned long long least = (unsigned long long)ceil(goal);
+            const Place p = find([least](uint32_t, unsigned long long x) { return x >= least; }, listed);
+            if (F32 && lost) return false;
             if (p.there) {
                 const double more = p.each ? ceil((goal - (double)p.mass) / (double)p.each) : 1.0;
                 const uint32_t in = (uint32_t)fmin(fmax(more, 1.0), (double)p.equal);
@@ -757,73 +839,106 @@ struct Chooser {
         }
         const uint32_t n_min = ask.min_p > 0.f ? max(s.n_min, 1u) : 0xffffffffu;
         if (n_min < n) first_tokens(n_min);
-        const double goal = (ask.u >= 0.f ? (double)ask.u : 0.0) * (double)kept;
-        Place p = find([goal](uint32_t, unsigned long long x) { return (double)x > goal; }, rare);
+        if (F32 && lost) return false;
+        const double goal = (ask.u >= 0.f ? fmin((double)ask.u, 1.0) : 0.0) * (double)kept;
+        const unsigned long long below = (unsigned long long)goal;
+        Place p = find([below](uint32_t, unsigned long long x) { return x > below; }, listed);
+        if (F32 && lost) return false;
         if (p.there && p.before < n) {
             out.nth = p.each ? (uint32_t)fmin(fmax(floor((goal - (double)p.mass) / (double)p.each), 0.0), (double)(p.equal - 1)) : 0u;
             out.nth = min(out.nth, n - 1 - p.before);
         } else {        // the last one of any weight
             const unsigned long long all = kept;
-            p = find([all](uint32_t, unsigned long long x) { return x >= all; }, rare);
+            p = find([all](uint32_t, unsigned long long x) { return x >= all; }, listed);
+            if (F32 && lost) return false;
             out.nth = (uint32_t)((kept - p.mass - 1) / p.each);
         }
-        if (rare) out.nth = s.owner;
-        out.pattern = p.key;
-        out.rare = rare;
+        if (listed) out.nth = s.owner;
+        out.key = p.key;
+        out.listed = listed;
         out.none = false;
-        out.y = ((double)pattern_value(p.key) - (double)m) * inv_t;
-        out.whole = whole;
-        out.kept = kept;
+        if (threadIdx.x == kRowThreads - 1) log_probs(a, r, ((double)key_value(p.key) - (double)m) * inv_t, whole, kept);     // (while the token is looked for)
         return true;
     }
 };
 
 __device__ __forceinline__ void clear_choice(ChooseLds &s)
 {
-    if (threadIdx.x < 64) s.runs[threadIdx.x] = 0;
+    if (threadIdx.x < kMostParts) s.zeros[threadIdx.x] = 0;
+    if (threadIdx.x < kRuns) s.runs[threadIdx.x] = 0;
     if (threadIdx.x == 0) {
-        s.rare = s.zeros = s.flags = s.n_min = s.sorted = 0;
-        s.rare_count[0] = s.rare_count[1] = 0;
+        s.rare[0] = s.rare[1] = s.flags = s.n_min = s.sorted[0] = s.sorted[1] = 0;
         s.rare_mass[0] = s.rare_mass[1] = 0;
-        s.rare_top[0] = 0;
-        s.rare_top[1] = 0xffffffffu;
+        s.top = s.gathered = 0xffffffffu;
     }
 }
 
-// The index of the nth token with that pattern among pieces [from, to), and the answer.  First the run of kRowThreads pieces, then the thread, then the element.
-__device__ __forceinline__ void answer(const SampleArgs &a, int r, const Row<false> &row, int from, int to, uint32_t nth, const Chosen &got, ChooseLds &s)
+// The index of the nth token with that pattern among pieces [from, to), at most NR runs of kRowThreads.  First the run, then the thread, then the element.
+template <int NR>
+__device__ __forceinline__ void answer(const SampleArgs &a, int r, const Row<false> &row, int from, int to, uint32_t nth, uint32_t pattern, ChooseLds &s)
 {
-    const uint32_t keep = got.pattern ? 0xffffu : 0x7fffu;      // (zeros of either sign)
-    const auto matches = [&](u32x4 w, int first) {
-        uint32_t n = 0;
+    static_assert(NR <= kRuns, "room for the runs");
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t keep = pattern ? 0xffffffffu : 0x7fff7fffu, both = pattern | pattern << 16;      // (zeros of either sign)
+    u32x4 w[NR];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            n |= (((e & 1 ? w[e >> 1] >> 16 : w[e >> 1]) & keep) == got.pattern && (unsigned)(first + e) < (unsigned)row.V ? 1u : 0u) << e;
-        return n;
+    for (int i = 0; i < NR; ++i) {
+        w[i] = u32x4{~both, ~both, ~both, ~both};
+        if (from + i * kRowThreads + tid < to) w[i] = row.base[from + i * kRowThreads + tid];
+    }
+    // the top bit of each half that matches
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+    const auto same = [&](uint32_t v) {
+        const uint32_t x = (v ^ both) & keep;
+        return __builtin_bit_cast(uint32_t, (u16x2)(__builtin_bit_cast(u16x2, x) - (u16x2){1, 1})) & ~x & 0x80008000u;
     };
-    for (int i = from + (int)threadIdx.x, run = 0; i < to; i += kRowThreads, ++run) {
-        const uint32_t n = __popc(matches(row.base[i], i * 8 - row.off));
-        if (n) atomicAdd(&s.runs[run], n);
+    const auto inside = [&](int i) {        // of the piece's eight elements those in the row
+        const int first = (from + i * kRowThreads + tid) * 8 - row.off;
+        return (first < 0 ? 0xffu << min(-first, 8) : 0xffu) & (first + 8 > row.V ? 0xffu >> min(first + 8 - row.V, 8) : 0xffu);
+    };
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        uint32_t n = __popc(same(w[i][0])) + __popc(same(w[i][1])) + __popc(same(w[i][2])) + __popc(same(w[i][3]));
+        if (n) {
+            const uint32_t in = inside(i);
+            if (in != 0xffu) {
+                n = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) n += (same(w[i][e >> 1]) >> (e & 1 ? 31 : 15) & in >> e) & 1u;
+            }
+            if (n) atomicAdd(&s.runs[i], n);
+        }
     }
     __syncthreads();
     int run = 0;
-    while (run < 63 && nth >= s.runs[run]) nth -= s.runs[run++];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = from + run * kRowThreads + (int)threadIdx.x;
-    const uint32_t bits = i < to ? matches(row.base[i], i * 8 - row.off) : 0u, in = __popc(bits);
-    uint32_t upto = in;
+    u32x4 its = w[0];
+    uint32_t count = s.runs[0];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t up = __shfl_up(upto, o, 64);
-        if (lane >= o) upto += up;
+    for (int i = 1; i < NR; ++i) {
+        const uint32_t here = s.runs[i];
+        if (run == i - 1 && nth >= count) {
+            nth -= count;
+            count = here;
+            run = i;
+            its = w[i];
+        }
     }
+    uint32_t mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t m = same(its[e]);
+        mine |= (m >> 15 & 1u) << (2 * e) | (m >> 31) << (2 * e + 1);
+    }
+    mine &= inside(run);
+    const uint32_t in = (uint32_t)__popc(mine), upto = scan_lanes<true>(in);
     if (lane == 63) s.wave_first[wave] = upto;
     __syncthreads();
-    uint32_t before = upto - in;
-    for (int j = 0; j < wave; ++j) before += s.wave_first[j];
+    const uint32_t wc = s.wave_first[lane & (kRowWaves - 1)], wcs = scan_lanes<false>(wc);
+    const int at = __builtin_amdgcn_readfirstlane(wave);
+    const uint32_t before = upto - in + lane_of(wcs, at) - lane_of(wc, at);
     if (nth >= before && nth < before + in) {
-        uint32_t left = bits;
-        for (uint32_t j = before; j < nth; ++j) left &= left - 1;
-        give(a, r, i * 8 - row.off + __ffs((int)left) - 1, got.y, got.whole, got.kept);
+        for (uint32_t j = before; j < nth; ++j) mine &= mine - 1;
+        a.token[r] = (from + run * kRowThreads + tid) * 8 - row.off + __ffs((int)mine) - 1;
     }
 }
 
@@ -846,56 +961,311 @@ __global__ __launch_bounds__(kRowThreads) void sample_values_kernel(SampleArgs a
         }
     };
     load(0);
+    const RowAsk ask = row_ask(a, r);
     for (int i = tid; i < kSide; i += kRowThreads) ((u32x4 *)s.bins)[i] = u32x4{0, 0, 0, 0};
     clear_choice(s);
     __syncthreads();
-    uint32_t zeros = 0, flags = 0;
+    Counts counts{nullptr, s.rare, s.list[0], kRare, 0, 0};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (q < 3) load(q + 1);
+        counts.bins = s.bins[q >> 1];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             const int in = i * kRowThreads + tid;
-            if (in < quarter) count_piece(w[q & 1][i], (q * quarter + in) * 8 - row.off, a.V, s.bins[q >> 1], q & 1 ? 65536u : 1u, s, zeros, flags);
+            if (in < quarter) counts.piece(w[q & 1][i], (q * quarter + in) * 8 - row.off, a.V, q & 1 ? 65536u : 1u);
+        }
+        if (counts.zeros) atomicAdd(&s.zeros[q], counts.zeros);
+        counts.zeros = 0;
+    }
+    if (counts.flags) atomicOr(&s.flags, counts.flags);
+    __syncthreads();
+    Chooser<false> x{s, row};
+    {
+        const bool negative = tid >= kRowThreads / 2;
+        const int size = negative ? (tid - kRowThreads / 2) * 4 : kSide - 4 - tid * 4;      // of the smallest of the thread's four
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 2 * (size + (negative ? i : 3 - i)) + negative;
+            const uint32_t lo = s.bins[0][at], hi = s.bins[1][at];
+            x.c[i] = (lo & 0xffffu) + (lo >> 16) + (hi & 0xffffu) + (hi >> 16);
         }
     }
-    if (zeros) atomicAdd(&s.zeros, zeros);
-    if (flags) atomicOr(&s.flags, flags);
-    __syncthreads();
-    Chooser x{s};
-#pragma unroll
-    for (int i = 0; i < Chooser::kEach; ++i) {
-        const int at = bin_slot(tid * Chooser::kEach + i);
-        const uint32_t lo = s.bins[0][at], hi = s.bins[1][at];
-        x.c[i] = (lo & 0xffffu) + (lo >> 16) + (hi & 0xffffu) + (hi >> 16);
-    }
+    const uint32_t zeros[4] = {s.zeros[0], s.zeros[1], s.zeros[2], s.zeros[3]};
     Chosen got;
-    if (!x.choose(row_ask(a, r), got)) {
+    if (!x.choose(a, r, ask, zeros[0] + zeros[1] + zeros[2] + zeros[3], got)) {
         __syncthreads();
         sample_row<false>(a, r, ((ValueLds *)lds)->row);
         return;
     }
-    if (got.none || got.rare) {
+    if (got.none || got.listed) {
         if (tid == 0) {
             if (got.none) no_token(a, r);
-            else give(a, r, (int)got.nth, got.y, got.whole, got.kept);
+            else a.token[r] = (int)got.nth;
         }
         return;
     }
+    const uint32_t pattern = __float_as_uint(key_value(got.key)) >> 16;
+    const uint32_t at = pattern ? 2 * ((pattern & 0x7fffu) - kFirst) + (pattern >> 15) : 0, lo = s.bins[0][at], hi = s.bins[1][at];
+    const uint32_t n[3] = {pattern ? lo & 0xffffu : zeros[0], pattern ? lo >> 16 : zeros[1], pattern ? hi & 0xffffu : zeros[2]};
     uint32_t nth = got.nth;
     int q = 0;
-    if (got.pattern) {      // (zeros are not counted by quarters: all of the row is searched for them)
-        const uint32_t size = (got.pattern & 0x7fffu) - kFirst, at = 2 * size + (got.pattern >> 15);
-        const uint32_t lo = s.bins[0][at], hi = s.bins[1][at];
-        const uint32_t n[3] = {lo & 0xffffu, lo >> 16, hi & 0xffffu};
-        while (q < 3 && nth >= n[q]) nth -= n[q++];
-        answer(a, r, row, q * quarter, min((q + 1) * quarter, row.pieces), nth, got, s);
-    } else {
-        answer(a, r, row, 0, row.pieces, nth, got, s);
+    while (q < 3 && nth >= n[q]) nth -= n[q++];
+    answer<NQ>(a, r, row, q * quarter, min((q + 1) * quarter, row.pieces), nth, pattern, s);
+}
+
+// Few rows: each cut into parts, counted by workgroups of their own ...
+constexpr int kCountThreads = 512;
+__global__ __launch_bounds__(kCountThreads) void sample_count_kernel(SampleArgs a, int parts)
+{
+    __shared__ __align__(16) uint32_t bins[2 * kSide];
+    __shared__ unsigned long long list[2][kPartRare];
+    __shared__ uint32_t rare[2], zeros, flags;
+    const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = (int)threadIdx.x;
+    const Row<false> row(a.logits, a.stride, r, a.V);
+    const int per = (row.pieces + parts - 1) / parts, from = part * per, to = min(from + per, row.pieces);
+    constexpr int kAhead = 4;
+    u32x4 w[kAhead];
+    const auto load = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            w[i] = u32x4{kNone, kNone, kNone, kNone};
+            if (i0 + i * kCountThreads + tid < to) w[i] = row.base[i0 + i * kCountThreads + tid];
+        }
+    };
+    load(from);
+    for (int i = tid; i < kSide / 2; i += kCountThreads) ((u32x4 *)bins)[i] = u32x4{0, 0, 0, 0};
+    if (tid == 0) rare[0] = rare[1] = zeros = flags = 0;
+    __syncthreads();
+    Counts counts{bins, rare, list[0], kPartRare, 0, 0};
+    for (int i0 = from; i0 < to; i0 += kAhead * kCountThreads) {
+        if (i0 > from) load(i0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) counts.piece(w[i], (i0 + i * kCountThreads + tid) * 8 - row.off, a.V, 1u);
+    }
+    if (counts.zeros) atomicAdd(&zeros, counts.zeros);
+    if (counts.flags) atomicOr(&flags, counts.flags);
+    __syncthreads();
+    PartCounts &out = ((PartCounts *)a.ws)[blockIdx.x];
+    for (int i = tid; i < kSide / 4; i += kCountThreads) {      // eight counts of 16 bits
+        const u32x4 x = ((const u32x4 *)bins)[2 * i], y = ((const u32x4 *)bins)[2 * i + 1];
+        ((u32x4 *)out.count)[i] = u32x4{x[0] | x[1] << 16, x[2] | x[3] << 16, y[0] | y[1] << 16, y[2] | y[3] << 16};
+    }
+    if (tid == 0) *(u32x4 *)&out.zeros = u32x4{zeros, flags, rare[0], rare[1]};
+    static_assert(kCountThreads == 2 * kPartRare, "a thread for each entry");
+    const int sign = tid / kPartRare, at = tid % kPartRare;
+    if ((uint32_t)at < rare[sign]) out.list[sign][at] = list[sign][at];
+}
+
+// ... and put together by one, which chooses and looks for the token in the part that holds it
+template <int NR>
+__global__ __launch_bounds__(kRowThreads) void sample_choose_kernel(SampleArgs a, int parts)
+{
+    extern __shared__ __align__(16) char lds[];
+    ChooseLds &s = ((ValueLds *)lds)->choose;
+    const int r = blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Row<false> row(a.logits, a.stride, r, a.V);
+    const PartCounts *const of = (const PartCounts *)a.ws + (int64_t)r * parts;
+    const RowAsk ask = row_ask(a, r);
+    // everything is requested at once: a wavefront's parts' heads, the beginnings of their lists (what may not be there is not used), and thread i's four bins,
+    // the even or the odd ones of eight counts
+    constexpr int kWaveParts = kMostParts / kRowWaves;
+    u32x4 head[kWaveParts];     // zeros, flags, rare values of either sign
+    unsigned long long early[kWaveParts][2];
+#pragma unroll
+    for (int i = 0; i < kWaveParts; ++i) {
+        const int p = wave + i * kRowWaves;
+        head[i] = u32x4{0, 0, 0, 0};
+        early[i][0] = early[i][1] = 0;
+        if (p < parts) {
+            head[i] = *(const u32x4 *)&of[p].zeros;
+            early[i][0] = of[p].list[0][lane];
+            early[i][1] = of[p].list[1][lane];
+        }
+    }
+    const bool negative = tid >= kRowThreads / 2;
+    const int eight = negative ? tid - kRowThreads / 2 : kRowThreads / 2 - 1 - tid;
+    uint32_t c[4] = {0, 0, 0, 0};
+#pragma unroll 1
+    for (int p0 = 0; p0 < parts; p0 += 8) {
+        u32x4 w[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
+            w[p] = u32x4{0, 0, 0, 0};
+            if (p0 + p < parts) w[p] = ((const u32x4 *)of[p0 + p].count)[eight];
+        }
+        if (p0 == 0) clear_choice(s);
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] += negative ? w[p][i] >> 16 : w[p][i] & 0xffffu;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kWaveParts; ++j) {
+        const int p = wave + j * kRowWaves;
+        if (p >= parts) break;
+        if (lane == 0) {
+            s.zeros[p] = head[j][0];
+            if (head[j][1]) atomicOr(&s.flags, head[j][1]);
+        }
+#pragma unroll
+        for (int sign = 0; sign < 2; ++sign) {
+            const uint32_t n = head[j][2 + sign];
+            if (n == 0) continue;
+            uint32_t base = 0;
+            if (lane == 0) base = atomicAdd(&s.rare[sign], n <= (uint32_t)kPartRare ? n : (uint32_t)kRare + 1);
+            base = lane_of(base, 0);
+            if (n > (uint32_t)kPartRare) continue;
+            for (uint32_t i = lane; i < n; i += 64)
+                if (base + i < (uint32_t)kRare) s.list[sign][base + i] = i < 64 ? early[j][sign] : of[p].list[sign][i];
+        }
+    }
+    __syncthreads();
+    Chooser<false> x{s, row};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.c[i] = negative ? c[i] : c[3 - i];
+    const uint32_t zeros_here = lane < parts && lane < kMostParts ? s.zeros[lane & (kMostParts - 1)] : 0, zeros_upto = scan_lanes<true>(zeros_here);
+    Chosen got;
+    if (!x.choose(a, r, ask, lane_of(zeros_upto, 63), got)) {
+        __syncthreads();
+        sample_row<false>(a, r, ((ValueLds *)lds)->row);
+        return;
+    }
+    if (got.none || got.listed) {
+        if (tid == 0) {
+            if (got.none) no_token(a, r);
+            else a.token[r] = (int)got.nth;
+        }
+        return;
+    }
+    // the part: lane p has its tokens of that value
+    const uint32_t pattern = __float_as_uint(key_value(got.key)) >> 16;
+    uint32_t in = zeros_here;
+    if (pattern) in = lane < parts ? of[lane].count[2 * ((pattern & 0x7fffu) - kFirst) + (pattern >> 15)] : 0;
+    const uint32_t upto = scan_lanes<true>(in);
+    const int part = __ffsll((long long)__ballot(upto > got.nth)) - 1;
+    const int per = (row.pieces + parts - 1) / parts;
+    answer<NR>(a, r, row, part * per, min((part + 1) * per, row.pieces), got.nth - (lane_of(upto, part) - lane_of(in, part)), pattern, s);
+}
+
+// 32-bit logits: a workgroup takes a row, reads it for its largest logit, for the bins, and for the tokens of each bin that a place is sought in.
+__global__ __launch_bounds__(kRowThreads) void sample_floats_kernel(SampleArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    FloatLds &s = ((WideLds *)lds)->choose;
+    const int r = blockIdx.x, tid = (int)threadIdx.x;
+    const Row<true> row(a.logits, a.stride, r, a.V);
+    const RowAsk ask = row_ask(a, r);
+    for (int i = tid; i < kSide / 2; i += kRowThreads) {
+        ((u32x4 *)s.bins)[i] = u32x4{0, 0, 0, 0};
+        ((u32x4 *)s.mass)[2 * i] = ((u32x4 *)s.mass)[2 * i + 1] = u32x4{0, 0, 0, 0};
+    }
+    clear_choice(s);
+    __syncthreads();
+    {
+        uint32_t top = 0xffffffffu;
+        bool bad = false;
+        row.all([&](int, float z) {
+            bad |= !(z < __builtin_inff());
+            top = min(top, order_key(z));
+        });
+        atomicMin(&s.top, top);
+        if (bad) s.flags = kBad;
+    }
+    __syncthreads();
+    Chooser<true> x{s, row};
+    x.m = key_value(s.top);
+    if (s.flags || !(x.m > -__builtin_inff()) || !usable(ask.t)) {
+        if (tid == 0) no_token(a, r);
+        return;
+    }
+    x.inv_t = 1.0 / (double)ask.t;
+    __syncthreads();
+    uint32_t zeros = 0, flags = 0, above = 0;
+    row.all([&](int index, float z) {
+        const uint32_t bits = __float_as_uint(z), b = bits >> 16, rb = (b - kFirst) & 0xffffu;
+        if (z == -__builtin_inff()) return;
+        double w;
+        const unsigned long long units = x.weigh(z, w);
+        above += w >= (double)ask.min_p;
+        if ((rb & 0x7800u) == 0) {
+            const uint32_t slot = 2 * (rb & 0x7fffu) + (rb >> 15);
+            atomicAdd(&s.bins[0][slot], 1u);
+            if (units) atomicAdd(&s.mass[slot], units);
+        } else if ((bits & 0x7fffffffu) == 0) {
+            ++zeros;
+        } else if ((b & 0x7fffu) < kFirst) {
+            const uint32_t at = atomicAdd(&s.rare[b >> 15], 1u);
+            if (at < (uint32_t)kRare) s.list[b >> 15][at] = (unsigned long long)order_key(z) << 32 | (uint32_t)index;
+            atomicAdd(&s.rare_mass[b >> 15], units);
+        } else {
+            flags |= b & 0x8000u ? kLow : kHigh;
+        }
+    });
+    if (zeros) atomicAdd(&s.zeros[0], zeros);
+    if (flags) atomicOr(&s.flags, flags);
+    if (ask.min_p > 0.f && above) atomicAdd(&s.n_min, above);
+    __syncthreads();
+    {
+        const bool negative = tid >= kRowThreads / 2;
+        const int size = negative ? (tid - kRowThreads / 2) * 4 : kSide - 4 - tid * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 2 * (size + (negative ? i : 3 - i)) + negative;
+            x.c[i] = s.bins[0][at];
+            x.unit[i] = s.mass[at];
+        }
+    }
+    Chosen got;
+    if (!x.choose(a, r, ask, s.zeros[0], got)) {
+        __syncthreads();
+        sample_row<true>(a, r, ((WideLds *)lds)->row);
+        return;
+    }
+    if (got.listed) {
+        if (tid == 0) a.token[r] = (int)got.nth;
+        return;
+    }
+    // zeros: the nth of either sign, looked for run by run
+    uint32_t nth = got.nth;
+    for (int i0 = 0; i0 < row.pieces; i0 += kRowThreads) {
+        uint32_t bits = 0;
+        if (i0 + tid < row.pieces) row.piece(i0 + tid, [&](int index, float z) { bits |= (z == 0.f ? 1u : 0u) << ((index + row.off) & 3); });
+        const uint32_t in = (uint32_t)__popc(bits), upto = scan_lanes<true>(in);
+        const int lane = tid & 63, wave = tid >> 6;
+        __syncthreads();
+        if (lane == 63) s.wave_first[wave] = upto;
+        __syncthreads();
+        const uint32_t wc = s.wave_first[lane & (kRowWaves - 1)], wcs = scan_lanes<false>(wc), here = lane_of(wcs, kRowWaves - 1);
+        if (nth < here) {
+            const int at = __builtin_amdgcn_readfirstlane(wave);
+            const uint32_t before = upto - in + lane_of(wcs, at) - lane_of(wc, at);
+            if (nth >= before && nth < before + in) {
+                for (uint32_t j = before; j < nth; ++j) bits &= bits - 1;
+                a.token[r] = (i0 + tid) * 4 - row.off + __ffs((int)bits) - 1;
+            }
+            return;
+        }
+        nth -= here;
     }
 }
 
-size_t sample_ws_bytes(int, int) { return 0; }
+// Parts of a row: none where there are rows enough, or little of them.  (Rows of 151936, us, in 1 / 4 / 8 / 16 parts: 1 row 20.8 / 17.8 / 16.2 / 16.3, 32 rows 22.4 /
+// 19.7 / 17.7 / 19.0, 64 rows 22.0 / 20.5 / 19.7 / 22.0, 128 rows 23.9 / 24.0 / 25.9, 256 rows 28.2 / 33.5.)
+static int sample_parts(int T, int V)
+{
+    const int pieces = (V + 14) / 8;        // (a row may begin anywhere in its first piece)
+    int parts = T <= 96 ? min(8, pieces / 1024) : 1;
+    if (pieces > 4 * 5 * kRowThreads) parts = max(parts, (pieces + 8 * 512 - 1) / (8 * 512));       // longer than a workgroup takes
+    return parts > 1 ? min(parts, kMostParts) : 1;
+}
+
+size_t sample_ws_bytes(int T, int V)
+{
+    const int parts = sample_parts(T, V);
+    return parts > 1 ? (size_t)T * parts * sizeof(PartCounts) : 0;
+}
 
 template <int NQ>
 static int launch_values(const SampleArgs &a, hipStream_t s)
@@ -907,18 +1277,41 @@ static int launch_values(const SampleArgs &a, hipStream_t s)
     return check_hip(hipGetLastError(), "sample_values_kernel");
 }
 
+template <int NR>
+static int launch_choose(const SampleArgs &a, int parts, hipStream_t s)
+{
+    static LdsLimitOnce once;
+    int rc = raise_lds_limit((const void *)sample_choose_kernel<NR>, once, "sample_choose_kernel");
+    if (rc) return rc;
+    sample_choose_kernel<NR><<<dim3((unsigned)a.T), dim3(kRowThreads), sizeof(ValueLds), s>>>(a, parts);
+    return check_hip(hipGetLastError(), "sample_choose_kernel");
+}
+
 int launch_sample(const SampleArgs &a, hipStream_t s)
 {
-    const int quarter = ((a.V + 7 + 7) / 8 + 3) / 4;      // (a row may begin anywhere in its first piece)
-    if (!a.f32 && quarter <= kRowThreads) return launch_values<1>(a, s);
-    if (!a.f32 && quarter <= 2 * kRowThreads) return launch_values<2>(a, s);
-    if (!a.f32 && quarter <= 5 * kRowThreads) return launch_values<5>(a, s);
-    static LdsLimitOnce once[2];
-    int rc = raise_lds_limit(a.f32 ? (const void *)sample_rows_kernel<true> : (const void *)sample_rows_kernel<false>, once[a.f32 ? 1 : 0], "sample_rows_kernel");
-    if (rc) return rc;
-    if (a.f32) sample_rows_kernel<true><<<dim3((unsigned)a.T), dim3(kRowThreads), sizeof(RowLds), s>>>(a);
-    else sample_rows_kernel<false><<<dim3((unsigned)a.T), dim3(kRowThreads), sizeof(RowLds), s>>>(a);
-    return check_hip(hipGetLastError(), "sample_rows_kernel");
+    if (a.f32) {
+        static LdsLimitOnce once;
+        int rc = raise_lds_limit((const void *)sample_floats_kernel, once, "sample_floats_kernel");
+        if (rc) return rc;
+        sample_floats_kernel<<<dim3((unsigned)a.T), dim3(kRowThreads), sizeof(WideLds), s>>>(a);
+        return check_hip(hipGetLastError(), "sample_floats_kernel");
+    }
+    const int parts = sample_parts(a.T, a.V), pieces = (a.V + 14) / 8;
+    if (parts > 1) {
+        if ((int64_t)a.T * parts > 0x7fffffffLL) {
+            set_error("qarl_sample: %d rows exceed the grid limit", a.T);
+            return QARL_ERR_UNSUPPORTED;
+        }
+        sample_count_kernel<<<dim3((unsigned)(a.T * parts)), dim3(kCountThreads), 0, s>>>(a, parts);
+        int rc = check_hip(hipGetLastError(), "sample_count_kernel");
+        if (rc) return rc;
+        const int per = (pieces + parts - 1) / parts;
+        return per <= kRowThreads ? launch_choose<1>(a, parts, s) : per <= 4 * kRowThreads ? launch_choose<4>(a, parts, s) : launch_choose<kRuns>(a, parts, s);
+    }
+    const int quarter = (pieces + 3) / 4;
+    if (quarter <= kRowThreads) return launch_values<1>(a, s);
+    if (quarter <= 2 * kRowThreads) return launch_values<2>(a, s);
+    return launch_values<5>(a, s);
 }
 
 }  // namespace qarl
