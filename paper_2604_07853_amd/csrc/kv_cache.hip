@@ -88,23 +88,34 @@ int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, co
 // A workgroup takes kReadRows output rows.  Its first threads look their rows' sequences up (the last s with offsets[s] <= row) and
 // leave the page's first cache row in LDS; then all threads copy.
 // 8 x 18432 positions of e4m3, 458 MB: 93.8 us with 32 rows and cached accesses, 86.3 with 16 and accesses that bypass the caches (5.3 TB/s); 37 short
-// sequences, 39 MB: 9.5 us cached, 10.4 past the caches: those are for calls that would not stay in them.
-constexpr int kReadRows = 16;
+// sequences, 39 MB: 9.5 us cached, 10.4 past the caches: those are for calls that would not stay in them.  Calls of few rows take four a workgroup: more of them
+// wait for lengths and pages at once.
 constexpr int64_t kReadCached = (int64_t)64 << 20;
 
-template <int D, int FMT, bool NT>
+template <int D, int FMT, bool NT, int kReadRows>
 __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvArgs c, const int32_t *__restrict__ table, int64_t table_stride, int table_width,
                                                              const int32_t *__restrict__ offsets, int S, int64_t total,
                                                              uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out)
 {
     constexpr int kChunks = D / 8;
     __shared__ int64_t from[kReadRows];     // cache row of head 0, or -1
+    __shared__ int32_t every[kKvThreads + 1];           // the offset of every `step`-th sequence, and the end: the search begins in LDS
     const int64_t row0 = (int64_t)blockIdx.x * kReadRows;
+    const int step = (S + kKvThreads - 1) / kKvThreads;
+    for (int i = threadIdx.x; i <= kKvThreads; i += kKvThreads) every[i] = S > 0 ? offsets[min((int64_t)i * step, (int64_t)S)] : 0;
+    __syncthreads();
     if (threadIdx.x < kReadRows) {
         const int64_t row = row0 + threadIdx.x;
         int64_t at = -1;
-        if (row < total && S > 0 && row >= offsets[0] && row < offsets[S]) {
-            int lo = 0, hi = S;             // offsets[lo] <= row < offsets[hi]
+        if (row < total && S > 0 && row >= every[0] && row < every[kKvThreads]) {
+            int lo = 0, hi = kKvThreads;    // every[lo] <= row < every[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (every[mid] <= row) lo = mid;
+                else hi = mid;
+            }
+            hi = min(hi * step, S);         // offsets[lo] <= row < offsets[hi]
+            lo *= step;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (offsets[mid] <= row) lo = mid;
@@ -155,18 +166,20 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvArgs c, const int
 int launch_kv_read(const KvArgs &c, const int32_t *table, int64_t table_stride, int table_width, const int32_t *offsets, int S,
                    int64_t total, void *k_out, void *v_out, hipStream_t s)
 {
-    const int64_t blocks = (total + kReadRows - 1) / kReadRows;
+    const bool nt = total * c.kv_heads * c.head_dim * (c.fmt == QARL_KV_BF16 ? 8 : c.fmt == QARL_KV_E4M3 ? 6 : 5) > kReadCached;
+    const int rows = total <= 16384 && !nt ? 4 : 16;
+    const int64_t blocks = (total + rows - 1) / rows;
     if (blocks > 0x7fffffffLL) {
         set_error("qarl_kv_cache_read: %lld rows exceed the grid limit", (long long)total);
         return QARL_ERR_UNSUPPORTED;
     }
     const dim3 grid((unsigned)blocks), block(kKvThreads);
     uint16_t *ko = (uint16_t *)k_out, *vo = (uint16_t *)v_out;
-    const bool nt = total * c.kv_heads * c.head_dim * (c.fmt == QARL_KV_BF16 ? 8 : c.fmt == QARL_KV_E4M3 ? 6 : 5) > kReadCached;
-#define QARL_KV_READ(D, FMT, NT) kv_read_kernel<D, FMT, NT><<<grid, block, 0, s>>>(c, table, table_stride, table_width, offsets, S, total, ko, vo)
+#define QARL_KV_READ(D, FMT, NT, ROWS) kv_read_kernel<D, FMT, NT, ROWS><<<grid, block, 0, s>>>(c, table, table_stride, table_width, offsets, S, total, ko, vo)
 #define QARL_KV_READ_AS(D, FMT) \
-    if (nt) QARL_KV_READ(D, FMT, true); \
-    else QARL_KV_READ(D, FMT, false)
+    if (rows == 4) QARL_KV_READ(D, FMT, false, 4); \
+    else if (nt) QARL_KV_READ(D, FMT, true, 16); \
+    else QARL_KV_READ(D, FMT, false, 16)
 #define QARL_KV_READ_FROM(D) \
     if (c.fmt == QARL_KV_E4M3) { \
         QARL_KV_READ_AS(D, QARL_KV_E4M3); \

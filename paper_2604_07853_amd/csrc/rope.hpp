@@ -31,30 +31,59 @@ __device__ __forceinline__ float2 rope_turn(uint64_t turns, int64_t p, float amp
     return make_float2(((quarter + 1u) & 2u ? -cs : cs) * amplitude, (quarter & 2u ? -sn : sn) * amplitude);
 }
 
-// Sixteen elements of a head as two runs of eight: where they begin, for the c-th sixteen.  A rotated one holds eight pairs, 8 c .. 8 c + 7.
+// What a lane holds of a head: two runs of 16 bytes, E elements each, at `at`.  Lane c of a head's first rotary_dim / 2 E has E whole pairs; neighbouring lanes'
+// runs are neighbours.  `pair`: of the first pair of either run (HALF: the runs are the pairs' two halves, and the second number is not used).
 struct RopeRuns {
-    int at[2];
+    int at[2], pair[2];
     bool turned;
 };
-__device__ __forceinline__ RopeRuns rope_runs(int c, int rot, int layout)
+template <int E>
+__device__ __forceinline__ RopeRuns rope_runs(int c, int head_dim, int rot, int layout)
 {
-    const bool turned = 16 * c < rot, half = turned && layout == QARL_ROPE_HALF;
-    return RopeRuns{{half ? 8 * c : 16 * c, half ? rot / 2 + 8 * c : 16 * c + 8}, turned};
+    const int lanes = rot / (2 * E), rest = (head_dim - rot) / (2 * E), j = c - lanes;
+    RopeRuns r;
+    r.turned = c < lanes;
+    if (!r.turned) {
+        r.at[0] = rot + E * j;
+        r.at[1] = rot + E * (rest + j);
+        r.pair[0] = r.pair[1] = 0;
+    } else if (layout == QARL_ROPE_HALF) {
+        r.at[0] = r.pair[0] = r.pair[1] = E * c;
+        r.at[1] = rot / 2 + E * c;
+    } else {
+        r.at[0] = E * c;
+        r.at[1] = E * (c + lanes);
+        r.pair[0] = E / 2 * c;
+        r.pair[1] = E / 2 * (c + lanes);
+    }
+    return r;
 }
 
-// The sixteen values turned: y = (a cos - b sin, b cos + a sin) of each pair (a, b)
-__device__ __forceinline__ void rope_apply(float (&x)[16], const float2 (&t)[8], int layout)
+// The lane's cosines and sines, out of a token's
+template <int E>
+__device__ __forceinline__ void rope_turns(const float2 *turns, const RopeRuns &r, int layout, float2 (&t)[E])
+{
+#pragma unroll
+    for (int i = 0; i < E; ++i) t[i] = make_float2(1.f, 0.f);
+    if (!r.turned) return;
+#pragma unroll
+    for (int i = 0; i < E; ++i) t[i] = turns[layout == QARL_ROPE_HALF || i < E / 2 ? r.pair[0] + i : r.pair[1] + i - E / 2];
+}
+
+// The lane's values turned: y = (a cos - b sin, b cos + a sin) of each pair (a, b)
+template <int E>
+__device__ __forceinline__ void rope_apply(float (&x)[2 * E], const float2 (&t)[E], int layout)
 {
     if (layout == QARL_ROPE_HALF) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = x[i], b = x[8 + i];
+        for (int i = 0; i < E; ++i) {
+            const float a = x[i], b = x[E + i];
             x[i] = fmaf(a, t[i].x, -(b * t[i].y));
-            x[8 + i] = fmaf(b, t[i].x, a * t[i].y);
+            x[E + i] = fmaf(b, t[i].x, a * t[i].y);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < E; ++i) {
             const float a = x[2 * i], b = x[2 * i + 1];
             x[2 * i] = fmaf(a, t[i].x, -(b * t[i].y));
             x[2 * i + 1] = fmaf(b, t[i].x, a * t[i].y);
