@@ -51,13 +51,6 @@ __device__ __forceinline__ uint32_t only_finite_e4m3(uint32_t w)
     return w & ~((bad - (bad >> 7)) | bad);
 }
 
-// Four scale bytes of an e2m1 row with zeros for those of NaN
-__device__ __forceinline__ uint32_t no_nan_scales(uint32_t w)
-{
-    const uint32_t bad = ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u;     // the top bit of a byte: it is 0xff
-    return w & ~((bad - (bad >> 7)) | bad);
-}
-
 // fp32 -> bf16, nearest even, two per instruction
 __device__ __forceinline__ uint32_t pack2_bf16(float x, float y)
 {

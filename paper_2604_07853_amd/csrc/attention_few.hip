@@ -24,10 +24,45 @@ struct FewLayout {
     static constexpr int kHalf = kFewTile * kRowBytes;                   // bytes of a tile of keys
     static constexpr int kStage = 2 * kHalf + (E4M3 || E2M1 ? 256 : 0);  // keys, values, 32 + 32 scales (e2m1: four bytes each)
     static constexpr int kStageCopies = 2 * kCopies + (E4M3 || E2M1 ? 1 : 0);
-    static constexpr int kRing = kStage <= 5000 ? 4 : 2;                 // stages; about 64 KiB per workgroup, D = 128 in bf16 128
+    // stages; about 64 KiB per workgroup, D = 128 in bf16 128.  e2m1 35, four workgroups a CU: 64 sequences of 8000 positions 77 -> 72 us, 256 of 4096 126 -> 119 with
+    // two stages instead of four (three: 74 and 121).
+    static constexpr int kRing = E2M1 ? 2 : kStage <= 5000 ? 4 : 2;
+    static constexpr int kWide = E2M1 ? 4 * kFewTile * 4 : 0;            // a wavefront's scales of values as numbers
     // Chunk c of row r lies at chunk c ^ swz(r): 16 rows that are read at the same chunk spread over all banks
     __device__ static constexpr int swz(int r) { return (r / (256 / kRowBytes)) & (kChunks - 1); }
 };
+
+// The sequence with the `left`-th longest cache, by sixteenths of the longest: where a CU gets several (sequence, head)s one behind the other, the long ones begin
+// first, and none of them when the others are done.  (Which workgroup takes a sequence changes no result.  256 sequences of up to 18432, four heads: e4m3 516 -> 489 us,
+// e2m1 285 -> 271; with 256 (sequence, head)s, which all begin at once, it has cost 5 %.)
+constexpr int kMostOrdered = 512;
+__device__ __forceinline__ int nth_longest(const AttnArgs &a, unsigned left, int lane)
+{
+    const int at = (int)left;
+    constexpr int kSets = kMostOrdered / 64;
+    int len[kSets], top = 0;
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+        len[i] = i * 64 < a.S ? max(0, min(a.kv_lens[min(i * 64 + lane, a.S - 1)], a.max_kv_len)) : 0;
+        top = max(top, len[i]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+    const float unit = 16.f / (float)(top + 1);
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) len[i] = i * 64 + lane < a.S ? (int)((float)len[i] * unit) : -1;
+    for (int b = 16; b >= 0; --b) {
+#pragma unroll
+        for (int i = 0; i < kSets; ++i) {
+            if (i * 64 >= a.S) break;
+            const unsigned long long of = __ballot(len[i] == b);
+            const unsigned n = (unsigned)__popcll(of);
+            if (left < n) return i * 64 + __ffsll((long long)__ballot((of >> lane & 1ull) && (unsigned)__popcll(of & ((1ull << lane) - 1)) == left)) - 1;
+            left -= n;
+        }
+    }
+    return at;      // (does not happen: every sequence is in one of them)
+}
 
 template <int D, int FMT, int NR>
 __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_kernel(AttnArgs a, int chunk, AttnParts parts)
@@ -42,7 +77,8 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
     const unsigned per_split = (unsigned)a.S * (unsigned)Hkv;
     const int split = (int)(blockIdx.x / per_split);
     const unsigned sh = blockIdx.x - (unsigned)split * per_split;
-    const int s = (int)(sh / (unsigned)Hkv), h = (int)(sh - (unsigned)s * (unsigned)Hkv);
+    const int s_at = (int)(sh / (unsigned)Hkv), h = (int)(sh - (unsigned)s_at * (unsigned)Hkv);
+    const int s = __builtin_amdgcn_readfirstlane(per_split > 512 && a.S > 1 && a.S <= kMostOrdered ? nth_longest(a, (unsigned)s_at, lane) : s_at);
     const SeqRange sr = seq_range(a, s);
     if (over_long(a, sr)) {
         if (split == 0 && parts.splits > 0) {
@@ -61,7 +97,8 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
     const int shift = a.kv.page_shift;
 
     char *ring = lds + wave * (L::kRing * L::kStage);
-    int *pages = (int *)(lds + kFewWaves * L::kRing * L::kStage);        // page of every eight positions of the piece, -1: none
+    float *const v_scale = (float *)(lds + kFewWaves * L::kRing * L::kStage) + wave * (L::kWide / 4);       // e2m1: a tile's scales of values, [quarter][32]
+    int *pages = (int *)(lds + kFewWaves * (L::kRing * L::kStage + L::kWide));       // page of every eight positions of the piece, -1: none
     const int32_t *table = a.table + (int64_t)s * a.table_stride;
     for (int i = tid; i < tiles * (kFewTile / 8); i += kFewThreads) {
         const int pos = min(max(lo + 8 * i, begin), end - 1);            // positions outside are the nearest one's again
@@ -90,6 +127,10 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[r][ks]));   // here before copies are in flight (a later wait would include them)
     lds_barrier();
 
+    // this head's rows of page 0, and the bytes from page to page (below 2^32)
+    const char *const k_head = (const char *)a.kv.k + ((int64_t)h << shift) * L::kRowBytes, *const v_head = (const char *)a.kv.v + ((int64_t)h << shift) * L::kRowBytes;
+    const uint32_t page_rows = (uint32_t)Hkv << shift, page_bytes = page_rows * (uint32_t)L::kRowBytes;
+
     // Copies of tile t into a stage.  Eight neighbouring positions lie in one page; positions outside [begin, end), which may hold
     // anything, are not read: the nearest position inside is, again.
     auto fill = [&](int t, int slot) {
@@ -103,15 +144,14 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             const int logical = (lane % L::kChunks) ^ L::swz(r);
             int page;
             if (L::kRowsPerCopy <= 8) page = __builtin_amdgcn_readlane(pl, c * L::kRowsPerCopy);
-            else if (L::kRowsPerCopy == 16) page = lane < 32 ? __builtin_amdgcn_readlane(pl, c * 16) : __builtin_amdgcn_readlane(pl, c * 16 + 8);
-            else page = pages[t * 4 + (lane >> 4)];
-            const int64_t first = ((int64_t)max(page, 0) * Hkv + h) << shift;
-            const uint32_t in = (uint32_t)(min(max(pos0 + r, begin), end - 1) & ((1 << shift) - 1)) * (uint32_t)L::kRowBytes + (uint32_t)(logical * 16);
-            copy16_to_lds((const char *)a.kv.k + first * L::kRowBytes + in, to + c * 1024);
-            copy16_to_lds((const char *)a.kv.v + first * L::kRowBytes + in, to + L::kHalf + c * 1024);
+            else page = pages[t * 4 + (r >> 3)];
+            const uint32_t in = (uint32_t)(clamp_pos(pos0 + r, begin, end - 1) & ((1 << shift) - 1)) * (uint32_t)L::kRowBytes + (uint32_t)(logical * 16);
+            const uint64_t at = (uint64_t)(uint32_t)max(page, 0) * page_bytes + in;
+            copy16_to_lds(k_head + at, to + c * 1024);
+            copy16_to_lds(v_head + at, to + L::kHalf + c * 1024);
         }
         if (E4M3 || E2M1) {
-            const int64_t at = (((int64_t)max(pl, 0) * Hkv + h) << shift) + (min(max(pos0 + (lane & 31), begin), end - 1) & ((1 << shift) - 1));
+            const uint64_t at = (uint64_t)(uint32_t)max(pl, 0) * page_rows + (uint32_t)((h << shift) + (clamp_pos(pos0 + (lane & 31), begin, end - 1) & ((1 << shift) - 1)));
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((lane < 32 ? a.kv.k_scales : a.kv.v_scales) + at),
                                              (__attribute__((address_space(3))) void *)(to + 2 * L::kHalf), 4, 0, 0);
         }
@@ -195,10 +235,17 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             }
         }
         f32x4 vs[2];
-        u32x4 vb[2];        // e2m1: the four scales of a value's row, a byte each
+        float wide[2];      // e2m1: two scales of position lane / 2
+        if (E2M1) {
+            const uint32_t b = *(const uint16_t *)(st + 2 * L::kHalf + 128 + 2 * lane);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t byte = e ? b >> 8 : b & 0xffu;
+                wide[e] = byte == 255 ? __builtin_nanf("") : e2m1_scale(byte);
+            }
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if (E2M1) vb[u] = *(const u32x4 *)(st + 2 * L::kHalf + 128 + (u * 16 + 4 * q) * 4);
             f32x4 kscale = f32x4{c2, c2, c2, c2};
             if (E4M3) {
                 kscale = *(const f32x4 *)(st + 2 * L::kHalf + (u * 16 + 4 * q) * 4) * c2;
@@ -277,11 +324,11 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             }
             if (E2M1) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t fine = no_nan_scales(vb[e >> 2][e & 3]);
-                    bad |= fine != vb[e >> 2][e & 3];
-                    vb[e >> 2][e & 3] = fine;
-                }
+                for (int e = 0; e < 2; ++e)
+                    if (wide[e] != wide[e]) {
+                        wide[e] = 0.f;
+                        bad = true;
+                    }
             }
             rare |= __ballot(bad) != 0;
         }
@@ -295,7 +342,10 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
         }
         if (E2M1) {
             // A row's four quarters have scales of their own, which the probabilities take on: exact (powers of two), rounded to bf16 once as before.  A
-            // transposing read brings a lane its eight positions of two runs of 16 of D.
+            // transposing read brings a lane its eight positions of two runs of 16 of D.  (The scales as numbers through LDS: each is made once a wavefront, not by
+            // the 16 lanes that want it.)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v_scale[(2 * (lane & 1) + e) * kFewTile + (lane >> 1)] = wide[e];
             const int r = (m16 & 3) + 4 * q + 4 * (m16 & 4);
             const uint32_t at = (uint32_t)(uintptr_t)(LdsPtr)st + L::kHalf + r * L::kRowBytes + (L::swz(r) * 16) + (m16 >> 3) * 8;
             u32x2 w[L::kChunks];
@@ -313,18 +363,13 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                float sc[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t b = (vb[e >> 2][e & 3] >> (8 * g)) & 0xffu;
-                    sc[e] = b == 255 ? __builtin_nanf("") : e2m1_scale(b);
-                }
+                const f32x4 sc[2] = {*(const f32x4 *)(v_scale + g * kFewTile + 4 * q), *(const f32x4 *)(v_scale + g * kFewTile + 16 + 4 * q)};
                 bf16x8 pg[NR];
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     float t[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) t[e] = pv[n][e] * sc[e];
+                    for (int e = 0; e < 8; ++e) t[e] = pv[n][e] * sc[e >> 2][e & 3];
                     pg[n] = pack_bf16x8(t);
                 }
 #pragma unroll
@@ -459,7 +504,7 @@ static int launch_few_as(const AttnArgs &a, const AttnPlan &p, const AttnParts &
         set_error("qarl_paged_attention: %lld pieces exceed the grid limit", (long long)grid);
         return QARL_ERR_UNSUPPORTED;
     }
-    const int stream = kFewWaves * L::kRing * L::kStage + p.few_chunk / 8 * 4, join = kFewWaves * 16 * NR * (D + 4 + 2) * 4;
+    const int stream = kFewWaves * (L::kRing * L::kStage + L::kWide) + p.few_chunk / 8 * 4, join = kFewWaves * 16 * NR * (D + 4 + 2) * 4;
     int rc = raise_lds_limit((const void *)attention_few_kernel<D, FMT, NR>, once, "attention_few_kernel");
     if (rc) return rc;
     attention_few_kernel<D, FMT, NR><<<dim3((unsigned)grid), dim3(kFewThreads), stream > join ? stream : join, s>>>(a, p.few_chunk, parts);

@@ -292,3 +292,22 @@ def test_offsets_past_32_bits(q):
         a = q.qarl_paged_attention(query[:n], big, torch.tensor([[pages - 2, pages - 1]], dtype=torch.int32, device="cuda"), *args)["out"]
         b = q.qarl_paged_attention(query[:n], small, torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), *args)["out"]
         assert torch.equal(a, b) and a.isfinite().all() and a.abs().sum() > 0
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("S,kv_heads,lens", [(70, 8, "ragged"), (300, 2, "ragged"), (512, 2, "equal"), (513, 2, "ragged"), (129, 4, "bound"), (64, 9, "few")])
+def test_sequences_taken_in_the_order_of_their_lengths(q, fmt, S, kv_heads, lens):
+    """More (sequence, head)s than workgroups begin at once: each is worked on, once, whatever the lengths (idle slots, equal ones, a bound far above them)."""
+    import test_gpu_attention as base
+    g = torch.Generator().manual_seed(S)
+    n = torch.randint(0, 90, (S,), generator=g).tolist()
+    if lens == "equal":
+        n = [33] * S
+    if lens == "few":
+        n = [0] * (S - 2) + [1, 70]
+    seqs = [(1, v) for v in n]
+    m = make(q, seqs, 2 * kv_heads, kv_heads, 64, 16, S) if fmt == "fp4" else base.make(q, fmt, seqs, 2 * kv_heads, kv_heads, 64, 16, S)
+    out = torch.full((S, 2 * kv_heads, 64), math.nan, dtype=torch.bfloat16, device="cuda")
+    got = call(q, m, max_kv=100000 if lens == "bound" else None, out=out)
+    assert got["out"].isfinite().all()
+    check(m, got)
