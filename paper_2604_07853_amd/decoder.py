@@ -1,10 +1,11 @@
 """A decoder layer on the library's own kernels: what a rollout engine (a few tokens per call) and the learner's forward (whole prompts) run.
 
-    residual add + RMS norm -> q, k, v projection -> paged cache (written quantized or plain) -> attention over it -> o projection
+    residual add + RMS norm -> q, k, v projection -> rotary positions and paged cache (16, 8 or 4 bits) in one launch -> attention over it -> o projection
     -> residual add + RMS norm (its output also as the experts' e4m3 rows) -> router -> quantized experts
 
-The projections are the grouped GEMM with one expert, on bf16 rows: W4A16 weights.  Positions are the caller's: `rotate(q, k)`, called on the views of the
-new tokens' queries and keys before they are cached, applies what the model uses.  The router's logits are a plain library product.
+The projections are the grouped GEMM with one expert, on bf16 rows: W4A16 weights.  Positions: a `Rope` and the new tokens' `positions`, turned on the way into the
+cache; or `rotate(q, k)`, called on the views of the new tokens' queries and keys before they are cached, applies whatever else the model uses.  The router's
+logits are a plain library product.
 """
 import torch
 
@@ -85,20 +86,26 @@ class DecoderLayer:
         return q.qarl_qgemm_grouped(self.dn, aq, r.offsets, M, x_scales=sa, epilogue=q.QARL_EPI_COMBINE, combine_w=r.w, sorted_pairs=r.pairs, T=T,
                                     topk=self.topk, path=q.QARL_PATH_PREFILL)
 
-    def forward(self, x, residual, slots, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, window=0, rotate=None):
+    def forward(self, x, residual, slots, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, window=0, rotate=None, rope=None, positions=None):
         """x [T, H] bf16: what the layer before has computed; residual [T, H]: the residual stream so far (None in front of the first layer).  slots,
-        block_table, kv_lens, q_offsets, max_q_len, max_kv_len: as for qarl_kv_cache_write and qarl_paged_attention, kv_lens with the new tokens.
+        block_table, kv_lens, q_offsets, max_q_len, max_kv_len: as for qarl_kv_cache_write and qarl_paged_attention, kv_lens with the new tokens.  rope, positions
+        [T]: as for qarl_rotary_kv_write, together; rotate (before them): any other function of the queries and keys.
         Returns (output, residual) for the next layer, whose first norm adds them.  Up to 512 tokens the output is the layer's own buffer, written
         again by its next call of up to 512, on whatever stream: such calls wait for the stream of the call before (and for its reader there); the replays
         of a captured step and other calls are for the caller to order."""
         T, c = x.shape[0], self.cache
+        if (rope is None) != (positions is None):
+            raise ValueError("rope and positions go together")
         n1 = q.qarl_add_rmsnorm(x, self.norm1, self.eps, residual=residual)
         residual = x if residual is None else n1["residual"]
         heads = self._project(self.qkv, n1["y"]).view(T, self.heads + 2 * c.kv_heads, c.head_dim)
         query, key, value = heads.split([self.heads, c.kv_heads, c.kv_heads], 1)
         if rotate is not None:
             query, key = rotate(query, key)
-        q.qarl_kv_cache_write(c, key, value, slots)
+        if rope is not None:
+            query = q.qarl_rotary_kv_write(c, rope, positions, query, key, value, slots, q_out=query if rotate is None else None)      # (the projection's rows are this call's own)
+        else:
+            q.qarl_kv_cache_write(c, key, value, slots)
         att = q.qarl_paged_attention(query, c, block_table, kv_lens, q_offsets, max_q_len, max_kv_len, window=window)["out"]
         out = self._project(self.o, att.view(T, self.heads * c.head_dim))
         # whole prompts on e4m3 rows: the norm quantizes them on the way, to the bytes that the decode path makes of its bf16 rows
