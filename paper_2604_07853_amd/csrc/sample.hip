@@ -434,6 +434,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, int r, RowLds &s
 constexpr uint32_t kFirst = 118 << 7;       // 2^-9
 constexpr double kLowest = 128.0;           // 2^7: sixteen powers of two on
 constexpr int kSide = 2048;                 // bins of a sign
+constexpr int kSlots = 2 * kSide;           // of both, by size, the signs side by side
 constexpr int kRare = 1024;                 // room for values of a sign below 2^-9 other than zero (one of 2800 tokens of logits that spread by 2.2)
 constexpr uint32_t kNone = 0xff80ff80u;     // two -inf
 constexpr int kMostParts = 32, kPartRare = 256, kRuns = 8;
@@ -447,7 +448,7 @@ struct PartCounts {
 };
 
 struct ChooseLds {
-    uint32_t bins[2][2 * kSide];            // a row's quarters, two to a word (row by row); the first half: a part's counts
+    uint32_t bins[2][kSlots];               // a row's quarters, two to a word (row by row); the first half: a part's counts
     unsigned long long list[3][kRare];      // the rare values by sign: key and index; 32-bit logits: those of one bin
     unsigned long long wave_mass[kRowWaves], rare_mass[2], rare_sum[kRowWaves];
     uint32_t wave_count[kRowWaves], wave_first[kRowWaves], wave_hit[2][kRowWaves];
@@ -511,7 +512,7 @@ __device__ __forceinline__ unsigned long long lane_of(unsigned long long v, int 
     return (unsigned long long)lane_of((uint32_t)(v >> 32), lane) << 32 | lane_of((uint32_t)v, lane);
 }
 
-// Two values into the bins (`bump` to be added to their counts), or to what is kept of others
+// Eight values into the bins (`bump` to be added to their counts), or to what is kept of others
 struct Counts {
     uint32_t *bins, *rare;
     unsigned long long *list;
@@ -523,16 +524,16 @@ struct Counts {
         const uint32_t slot = __builtin_bit_cast(uint32_t, (u16x2)(r << 1)) | __builtin_bit_cast(uint32_t, (u16x2)(r >> 15));
         const uint32_t rw = __builtin_bit_cast(uint32_t, r);
         if ((rw & 0x78007800u) == 0) {
-            atomicAdd((uint32_t *)((char *)bins + ((slot << 2) & 0x3fffcu)), bump);
-            atomicAdd((uint32_t *)((char *)bins + ((slot >> 14) & 0x3fffcu)), bump);
+            atomicAdd(bins + (slot & 0xffffu), bump);
+            atomicAdd(bins + (slot >> 16), bump);
             return;
         }
         if (w == kNone) return;
-#pragma unroll
+#pragma unroll 1
         for (int e = 0; e < 2; ++e) {
-            const uint32_t b = e ? w >> 16 : w & 0xffffu, rb = e ? rw >> 16 : rw & 0xffffu, size = b & 0x7fffu;
-            if ((rb & 0x7800u) == 0) {
-                atomicAdd(bins + (e ? slot >> 16 : slot & 0xffffu), bump);
+            const uint32_t b = (w >> 16 * e) & 0xffffu, size = b & 0x7fffu;
+            if (((b - kFirst) & 0x7800u) == 0) {
+                atomicAdd(bins + ((slot >> 16 * e) & 0xffffu), bump);
             } else if (size == 0) {
                 ++zeros;
             } else if (size < kFirst) {
@@ -543,10 +544,9 @@ struct Counts {
             }
         }
     }
-    // Eight values; those outside the row become -inf
     __device__ __forceinline__ void piece(u32x4 w, int first, int V, uint32_t bump)
     {
-        if (first < 0 || first + 8 > V) {
+        if (first < 0 || first + 8 > V) {       // those outside the row become -inf
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if ((unsigned)(first + e) >= (unsigned)V) w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | (kNone & 0xffff0000u) : (w[e >> 1] & 0xffff0000u) | (kNone & 0xffffu);
@@ -952,31 +952,35 @@ __global__ __launch_bounds__(kRowThreads) void sample_values_kernel(SampleArgs a
     const Row<false> row(a.logits, a.stride, r, a.V);
     const int quarter = (row.pieces + 3) / 4;
     u32x4 w[2][NQ];
-    const auto load = [&](int q) {
+    const auto load = [&](int q, int to) {
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             const int in = i * kRowThreads + tid;
-            w[q & 1][i] = u32x4{kNone, kNone, kNone, kNone};
-            if (in < quarter && q * quarter + in < row.pieces) w[q & 1][i] = row.base[q * quarter + in];
+            w[to][i] = u32x4{kNone, kNone, kNone, kNone};
+            if (in < quarter && q * quarter + in < row.pieces) w[to][i] = row.base[q * quarter + in];
         }
     };
-    load(0);
+    load(0, 0);
     const RowAsk ask = row_ask(a, r);
-    for (int i = tid; i < kSide; i += kRowThreads) ((u32x4 *)s.bins)[i] = u32x4{0, 0, 0, 0};
+    for (int i = tid; i < 2 * kSlots / 4; i += kRowThreads) ((u32x4 *)s.bins)[i] = u32x4{0, 0, 0, 0};
     clear_choice(s);
     __syncthreads();
     Counts counts{nullptr, s.rare, s.list[0], kRare, 0, 0};
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {      // (a loop: the way of every piece is long, and the instruction cache small)
+        counts.bins = s.bins[half];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (q < 3) load(q + 1);
-        counts.bins = s.bins[q >> 1];
+        for (int odd = 0; odd < 2; ++odd) {
+            const int q = 2 * half + odd;
+            if (q < 3) load(q + 1, odd ^ 1);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const int in = i * kRowThreads + tid;
-            if (in < quarter) counts.piece(w[q & 1][i], (q * quarter + in) * 8 - row.off, a.V, q & 1 ? 65536u : 1u);
+            for (int i = 0; i < NQ; ++i) {
+                const int in = i * kRowThreads + tid;
+                if (in < quarter) counts.piece(w[odd][i], (q * quarter + in) * 8 - row.off, a.V, odd ? 65536u : 1u);
+            }
+            if (counts.zeros) atomicAdd(&s.zeros[q], counts.zeros);
+            counts.zeros = 0;
         }
-        if (counts.zeros) atomicAdd(&s.zeros[q], counts.zeros);
-        counts.zeros = 0;
     }
     if (counts.flags) atomicOr(&s.flags, counts.flags);
     __syncthreads();
@@ -1018,7 +1022,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_values_kernel(SampleArgs a
 constexpr int kCountThreads = 512;
 __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(SampleArgs a, int parts)
 {
-    __shared__ __align__(16) uint32_t bins[2 * kSide];
+    __shared__ __align__(16) uint32_t bins[kSlots];
     __shared__ unsigned long long list[2][kPartRare];
     __shared__ uint32_t rare[2], zeros, flags;
     const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = (int)threadIdx.x;
