@@ -11,6 +11,8 @@
 // 16-bit logits have few values: 4096 bins hold those of size 2^-9 to 2^7 one by one, so that a count says all of a bin, weights are computed once a value
 // and not once a token, and a place in the order is a bin and a number.  32-bit logits are put into the same bins by their upper halves: these get weights beside
 // their counts, and the tokens of a bin that a place lies in are gathered and sorted.  Rows whose other values matter take a general way, which asks for nothing.
+#include <stddef.h>
+
 #include <type_traits>
 
 #include "common.hpp"
@@ -56,20 +58,23 @@ struct Row {
             if ((unsigned)(first + e) < (unsigned)V) f(first + e, z);
         }
     }
+    // ... of pieces [from, to), the workgroup together
     template <typename Fn>
-    __device__ __forceinline__ void all(Fn f) const
+    __device__ __forceinline__ void span(int from, int to, Fn f) const
     {
         constexpr int kAhead = 4;       // pieces requested at once
-        for (int i = threadIdx.x; i < pieces; i += kAhead * kRowThreads) {
+        for (int i = from + (int)threadIdx.x; i < to; i += kAhead * kRowThreads) {
             u32x4 w[kAhead];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
-                if (i + j * kRowThreads < pieces) w[j] = base[i + j * kRowThreads];
+                if (i + j * kRowThreads < to) w[j] = base[i + j * kRowThreads];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
-                if (i + j * kRowThreads < pieces) elements(i + j * kRowThreads, w[j], f);
+                if (i + j * kRowThreads < to) elements(i + j * kRowThreads, w[j], f);
         }
     }
+    template <typename Fn>
+    __device__ __forceinline__ void all(Fn f) const { span(0, pieces, f); }
 };
 
 // (2^52 added: the sum's last bit is a unit)
@@ -452,7 +457,7 @@ struct ChooseLds {
     unsigned long long list[3][kRare];      // the rare values by sign: key and index; 32-bit logits: those of one bin
     unsigned long long wave_mass[kRowWaves], rare_mass[2], rare_sum[kRowWaves];
     uint32_t wave_count[kRowWaves], wave_first[kRowWaves], wave_hit[2][kRowWaves];
-    uint32_t rare[2], sorted[2], flags, n_min, top, zeros[kMostParts], gathered, in_bin, bin_sorted;
+    uint32_t rare[2], sorted[2], flags, n_min, top, zeros[kMostParts], in_bin, bin_sorted;
     uint32_t runs[kRuns];
     Place place[2][kRowWaves], spot;
     uint32_t owner;
@@ -463,6 +468,7 @@ union ValueLds {
 };
 struct FloatLds : ChooseLds {
     unsigned long long mass[2 * kSide];
+    double powers[64];      // 2^(j / 64)
 };
 union WideLds {
     FloatLds choose;
@@ -576,14 +582,36 @@ struct Chooser {
     float m;
     double inv_t;
     int calls;
+    uint32_t gathered;                          // 32-bit logits: the bin whose tokens are in the third list
     bool lost;                                  // 32-bit logits: a bin's tokens are more than there is room for
 
-    __device__ __forceinline__ unsigned long long weigh(float z, double &w) const { return weight_of(((double)z - (double)m) * inv_t, w); }
+    // 32-bit logits are weighed one by one: y = k ln 2 / 64 + r, the power series of e^r up to r^4 within 4e-14, 2^(k / 64) out of a table.  (y below -31: no unit.)
+    __device__ static __forceinline__ unsigned long long weigh_by(const Lds &s, double y, double &w)
+    {
+        if constexpr (!F32) return weight_of(y, w);
+        else {
+            if (!(y > -31.5)) {
+                w = 0.0;
+                return 0;
+            }
+            const double kd = rint(y * 92.332482616893656877);
+            const double r = fma(-kd, 0.010830424696249145, y);
+            const int k = (int)kd;
+            double p = fma(1.0 / 24.0, r, 1.0 / 6.0);
+            p = fma(p, r, 0.5);
+            p = fma(p, r, 1.0);
+            p = fma(p, r, 1.0);
+            p *= s.powers[k & 63];
+            w = __longlong_as_double(__double_as_longlong(p) + ((long long)(k >> 6) << 52));
+            return weight_units(w);
+        }
+    }
+    __device__ __forceinline__ unsigned long long weigh(float z, double &w) const { return weigh_by(s, ((double)z - (double)m) * inv_t, w); }
 
     // The place among the n <= kRowThreads tokens of a list of keys and indices, each a bin of its own: sorted the first time that one is asked for.
     // (The result in s.spot, its index in s.owner.  A function of its own: it is seldom called, and costs the others registers.)
     template <typename Fn>
-    __device__ static __attribute__((noinline)) void among(ChooseLds &s, unsigned long long *list, uint32_t n, uint32_t *sorted, uint32_t before, unsigned long long mass, float m,
+    __device__ static __attribute__((noinline)) void among(Lds &s, unsigned long long *list, uint32_t n, uint32_t *sorted, uint32_t before, unsigned long long mass, float m,
                                                            double inv_t, Fn pass)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -614,13 +642,14 @@ struct Chooser {
             index = (uint32_t)list[threadIdx.x];
             key = (uint32_t)(list[threadIdx.x] >> 32);
             double w;
-            u = weight_of(((double)key_value(key) - (double)m) * inv_t, w);
+            u = weigh_by(s, ((double)key_value(key) - (double)m) * inv_t, w);
         }
         const unsigned long long upto = scan_lanes<true>(u);
         if (lane == 63) s.rare_sum[wave] = upto;
         __syncthreads();
-        mass += upto - u;
-        for (int i = 0; i < wave; ++i) mass += s.rare_sum[i];
+        const unsigned long long sums = s.rare_sum[lane & (kRowWaves - 1)], sums_upto = scan_lanes<false>(sums);
+        const int at = __builtin_amdgcn_readfirstlane(wave);
+        mass += upto - u + lane_of(sums_upto, at) - lane_of(sums, at);
         before += threadIdx.x;
         // the first that passes: what stands in front of it does not
         if (threadIdx.x < n && pass(before + 1, mass + u) && (threadIdx.x == 0 || !pass(before, mass))) {
@@ -630,17 +659,12 @@ struct Chooser {
         __syncthreads();
     }
 
-    // 32-bit logits: the tokens of a bin into the third list
+    // 32-bit logits: the tokens of a bin into the third list.  (The last that was done with the list ended with a barrier.)
     __device__ __forceinline__ void gather(uint32_t pattern)
     {
-        __syncthreads();
-        if (s.gathered == pattern) return;      // (they are there)
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            s.gathered = pattern;
-            s.in_bin = 0;
-            s.bin_sorted = 0;
-        }
+        if (gathered == pattern) return;        // (they are there)
+        gathered = pattern;
+        if (threadIdx.x == 0) s.in_bin = s.bin_sorted = 0;
         __syncthreads();
         row.all([&](int index, float z) {
             if (__float_as_uint(z) >> 16 == pattern) {
@@ -711,6 +735,7 @@ struct Chooser {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & (kRowWaves - 1);
         calls = 0;
         lost = false;
+        gathered = 0xffffffffu;
         const uint32_t n_rare[2] = {min(s.rare[0], (uint32_t)kRare), min(s.rare[1], (uint32_t)kRare)};
         double w = 0.0;
         uint32_t csum = 0;
@@ -869,7 +894,7 @@ __device__ __forceinline__ void clear_choice(ChooseLds &s)
     if (threadIdx.x == 0) {
         s.rare[0] = s.rare[1] = s.flags = s.n_min = s.sorted[0] = s.sorted[1] = 0;
         s.rare_mass[0] = s.rare_mass[1] = 0;
-        s.top = s.gathered = 0xffffffffu;
+        s.top = 0xffffffffu;
     }
 }
 
@@ -1153,46 +1178,33 @@ __global__ __launch_bounds__(kRowThreads) void sample_choose_kernel(SampleArgs a
     answer<NR>(a, r, row, part * per, min((part + 1) * per, row.pieces), got.nth - (lane_of(upto, part) - lane_of(in, part)), pattern, s);
 }
 
-// 32-bit logits: a workgroup takes a row, reads it for its largest logit, for the bins, and for the tokens of each bin that a place is sought in.
-__global__ __launch_bounds__(kRowThreads) void sample_floats_kernel(SampleArgs a)
+// ---- 32-bit logits: a row is read for its largest logit, for the bins, and for the tokens of each bin that a place is sought in.
+
+// Pieces [from, to): the key of the largest logit into s.top, and whether there is a NaN or +inf into s.flags
+__device__ __forceinline__ void float_top(const Row<true> &row, int from, int to, FloatLds &s)
 {
-    extern __shared__ __align__(16) char lds[];
-    FloatLds &s = ((WideLds *)lds)->choose;
-    const int r = blockIdx.x, tid = (int)threadIdx.x;
-    const Row<true> row(a.logits, a.stride, r, a.V);
-    const RowAsk ask = row_ask(a, r);
-    for (int i = tid; i < kSide / 2; i += kRowThreads) {
-        ((u32x4 *)s.bins)[i] = u32x4{0, 0, 0, 0};
-        ((u32x4 *)s.mass)[2 * i] = ((u32x4 *)s.mass)[2 * i + 1] = u32x4{0, 0, 0, 0};
-    }
-    clear_choice(s);
-    __syncthreads();
-    {
-        uint32_t top = 0xffffffffu;
-        bool bad = false;
-        row.all([&](int, float z) {
-            bad |= !(z < __builtin_inff());
-            top = min(top, order_key(z));
-        });
-        atomicMin(&s.top, top);
-        if (bad) s.flags = kBad;
-    }
-    __syncthreads();
-    Chooser<true> x{s, row};
-    x.m = key_value(s.top);
-    if (s.flags || !(x.m > -__builtin_inff()) || !usable(ask.t)) {
-        if (tid == 0) no_token(a, r);
-        return;
-    }
-    x.inv_t = 1.0 / (double)ask.t;
-    __syncthreads();
+    uint32_t top = 0xffffffffu;
+    bool bad = false;
+    row.span(from, to, [&](int, float z) {
+        bad |= !(z < __builtin_inff());
+        top = min(top, order_key(z));
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = min(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    if ((threadIdx.x & 63) == 0) atomicMin(&s.top, top);
+    if (bad) s.flags = kBad;
+}
+
+// Pieces [from, to) into the bins
+__device__ __forceinline__ void float_bins(const Row<true> &row, int from, int to, float min_p, const Chooser<true> &x, FloatLds &s)
+{
     uint32_t zeros = 0, flags = 0, above = 0;
-    row.all([&](int index, float z) {
+    row.span(from, to, [&](int index, float z) {
         const uint32_t bits = __float_as_uint(z), b = bits >> 16, rb = (b - kFirst) & 0xffffu;
         if (z == -__builtin_inff()) return;
         double w;
         const unsigned long long units = x.weigh(z, w);
-        above += w >= (double)ask.min_p;
+        above += w >= (double)min_p;
         if ((rb & 0x7800u) == 0) {
             const uint32_t slot = 2 * (rb & 0x7fffu) + (rb >> 15);
             atomicAdd(&s.bins[0][slot], 1u);
@@ -1209,18 +1221,23 @@ __global__ __launch_bounds__(kRowThreads) void sample_floats_kernel(SampleArgs a
     });
     if (zeros) atomicAdd(&s.zeros[0], zeros);
     if (flags) atomicOr(&s.flags, flags);
-    if (ask.min_p > 0.f && above) atomicAdd(&s.n_min, above);
-    __syncthreads();
-    {
-        const bool negative = tid >= kRowThreads / 2;
-        const int size = negative ? (tid - kRowThreads / 2) * 4 : kSide - 4 - tid * 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = 2 * (size + (negative ? i : 3 - i)) + negative;
-            x.c[i] = s.bins[0][at];
-            x.unit[i] = s.mass[at];
-        }
+    if (min_p > 0.f && above) atomicAdd(&s.n_min, above);
+}
+
+__device__ __forceinline__ void clear_floats(FloatLds &s)
+{
+    for (int i = threadIdx.x; i < kSide / 2; i += kRowThreads) {
+        ((u32x4 *)s.bins)[i] = u32x4{0, 0, 0, 0};
+        ((u32x4 *)s.mass)[2 * i] = ((u32x4 *)s.mass)[2 * i + 1] = u32x4{0, 0, 0, 0};
     }
+    if (threadIdx.x < 64) s.powers[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
+    clear_choice(s);
+}
+
+// The choice out of the bins (thread i's counts and weights are in x) and what stands beside them in s
+__device__ __forceinline__ void float_choice(const SampleArgs &a, int r, const RowAsk &ask, const Row<true> &row, Chooser<true> &x, FloatLds &s, char *lds)
+{
+    const int tid = (int)threadIdx.x;
     Chosen got;
     if (!x.choose(a, r, ask, s.zeros[0], got)) {
         __syncthreads();
@@ -1255,6 +1272,171 @@ __global__ __launch_bounds__(kRowThreads) void sample_floats_kernel(SampleArgs a
     }
 }
 
+// slot of thread i's j-th bin
+__device__ __forceinline__ int own_slot(int j)
+{
+    const int tid = (int)threadIdx.x, negative = tid >= kRowThreads / 2;
+    return 2 * (negative ? (tid - kRowThreads / 2) * 4 + j : kSide - 1 - tid * 4 - j) + negative;
+}
+
+__global__ __launch_bounds__(kRowThreads) void sample_floats_kernel(SampleArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    FloatLds &s = ((WideLds *)lds)->choose;
+    const int r = blockIdx.x;
+    const Row<true> row(a.logits, a.stride, r, a.V);
+    const RowAsk ask = row_ask(a, r);
+    clear_floats(s);
+    __syncthreads();
+    float_top(row, 0, row.pieces, s);
+    __syncthreads();
+    Chooser<true> x{s, row};
+    x.m = key_value(s.top);
+    if (s.flags || !(x.m > -__builtin_inff()) || !usable(ask.t)) {
+        if (threadIdx.x == 0) no_token(a, r);
+        return;
+    }
+    x.inv_t = 1.0 / (double)ask.t;
+    __syncthreads();
+    float_bins(row, 0, row.pieces, ask.min_p, x, s);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x.c[i] = s.bins[0][own_slot(i)];
+        x.unit[i] = s.mass[own_slot(i)];
+    }
+    float_choice(a, r, ask, row, x, s, lds);
+}
+
+// Few rows: cut into parts.  The first kernel finds the parts' largest logits (and clears), the second adds what the parts' bins hold to the row's, the third
+// chooses.  Whole numbers are added: in whatever order, the sums are the same.
+struct FloatRow {
+    uint32_t count[2 * kSide];
+    unsigned long long mass[2 * kSide], rare_mass[2];
+    uint32_t zeros, flags, n_min, rare[2], unused[3];
+    uint32_t top[kMostParts], bad[kMostParts];
+    unsigned long long list[2][kRare];
+};
+
+__global__ __launch_bounds__(kRowThreads) void sample_float_tops_kernel(SampleArgs a, int parts)
+{
+    __shared__ uint32_t tops[kRowWaves], bads;
+    const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = (int)threadIdx.x;
+    const Row<true> row(a.logits, a.stride, r, a.V);
+    FloatRow &f = ((FloatRow *)a.ws)[r];
+    const int per = (row.pieces + parts - 1) / parts, from = part * per, to = min(from + per, row.pieces);
+    if (tid == 0) bads = 0;
+    __syncthreads();
+    uint32_t top = 0xffffffffu;
+    bool bad = false;
+    row.span(from, to, [&](int, float z) {
+        bad |= !(z < __builtin_inff());
+        top = min(top, order_key(z));
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = min(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    if (bad) bads = 1;
+    constexpr int kClear = (int)(offsetof(FloatRow, top) / 16);
+    static_assert(offsetof(FloatRow, top) % 16 == 0, "cleared in 16 bytes");
+    for (int i = part * kRowThreads + tid; i < kClear; i += parts * kRowThreads) ((u32x4 *)&f)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    if (tid == 0) {
+        for (int i = 1; i < kRowWaves; ++i) top = min(top, tops[i]);
+        f.top[part] = top;
+        f.bad[part] = bads;
+    }
+}
+
+// The largest logit of the row's parts; false: there is no distribution
+__device__ __forceinline__ bool row_top(const FloatRow &f, int parts, const RowAsk &ask, Chooser<true> &x)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t top = lane < parts ? f.top[lane & (kMostParts - 1)] : 0xffffffffu;
+    const bool bad = __ballot(lane < parts && f.bad[lane & (kMostParts - 1)]) != 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = min(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    x.m = key_value(top);
+    x.inv_t = 1.0 / (double)ask.t;
+    return !bad && x.m > -__builtin_inff() && usable(ask.t);
+}
+
+__global__ __launch_bounds__(kRowThreads) void sample_float_bins_kernel(SampleArgs a, int parts)
+{
+    extern __shared__ __align__(16) char lds[];
+    FloatLds &s = ((WideLds *)lds)->choose;
+    const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = (int)threadIdx.x;
+    const Row<true> row(a.logits, a.stride, r, a.V);
+    const RowAsk ask = row_ask(a, r);
+    FloatRow &f = ((FloatRow *)a.ws)[r];
+    const int per = (row.pieces + parts - 1) / parts, from = part * per, to = min(from + per, row.pieces);
+    Chooser<true> x{s, row};
+    if (!row_top(f, parts, ask, x)) return;
+    clear_floats(s);
+    __syncthreads();
+    float_bins(row, from, to, ask.min_p, x, s);
+    __syncthreads();
+    for (int i = tid; i < 2 * kSide; i += kRowThreads) {
+        const uint32_t n = s.bins[0][i];
+        if (n) {
+            atomicAdd(&f.count[i], n);
+            if (s.mass[i]) atomicAdd(&f.mass[i], s.mass[i]);
+        }
+    }
+    if (tid == 0) {
+        if (s.zeros[0]) atomicAdd(&f.zeros, s.zeros[0]);
+        if (s.flags) atomicOr(&f.flags, s.flags);
+        if (s.n_min) atomicAdd(&f.n_min, s.n_min);
+    }
+    if (tid < 2) {
+        const uint32_t n = s.rare[tid];
+        if (n) s.runs[tid] = atomicAdd(&f.rare[tid], n);
+        if (s.rare_mass[tid]) atomicAdd(&f.rare_mass[tid], s.rare_mass[tid]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int sign = 0; sign < 2; ++sign)
+        if ((uint32_t)tid < min(s.rare[sign], (uint32_t)kRare) && s.runs[sign] + tid < (uint32_t)kRare) f.list[sign][s.runs[sign] + tid] = s.list[sign][tid];
+}
+
+__global__ __launch_bounds__(kRowThreads) void sample_float_choose_kernel(SampleArgs a, int parts)
+{
+    extern __shared__ __align__(16) char lds[];
+    FloatLds &s = ((WideLds *)lds)->choose;
+    const int r = blockIdx.x, tid = (int)threadIdx.x;
+    const Row<true> row(a.logits, a.stride, r, a.V);
+    const RowAsk ask = row_ask(a, r);
+    const FloatRow &f = ((const FloatRow *)a.ws)[r];
+    Chooser<true> x{s, row};
+    if (!row_top(f, parts, ask, x)) {
+        if (tid == 0) no_token(a, r);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x.c[i] = f.count[own_slot(i)];
+        x.unit[i] = f.mass[own_slot(i)];
+    }
+    static_assert(kRare == kRowThreads, "a thread for each rare value");
+    const uint32_t rare[2] = {f.rare[0], f.rare[1]};
+    clear_floats(s);
+    __syncthreads();
+#pragma unroll
+    for (int sign = 0; sign < 2; ++sign)
+        if ((uint32_t)tid < rare[sign]) s.list[sign][tid] = f.list[sign][tid];
+    if (tid == 0) {
+        s.zeros[0] = f.zeros;
+        s.flags = f.flags;
+        s.n_min = f.n_min;
+        s.rare[0] = rare[0];
+        s.rare[1] = rare[1];
+        s.rare_mass[0] = f.rare_mass[0];
+        s.rare_mass[1] = f.rare_mass[1];
+    }
+    __syncthreads();
+    float_choice(a, r, ask, row, x, s, lds);
+}
+
 // Parts of a row: none where there are rows enough, or little of them.  (Rows of 151936, us, in 1 / 4 / 8 / 16 parts: 1 row 20.8 / 17.8 / 16.2 / 16.3, 32 rows 22.4 /
 // 19.7 / 17.7 / 19.0, 64 rows 22.0 / 20.5 / 19.7 / 22.0, 128 rows 23.9 / 24.0 / 25.9, 256 rows 28.2 / 33.5.)
 static int sample_parts(int T, int V)
@@ -1265,10 +1447,14 @@ static int sample_parts(int T, int V)
     return parts > 1 ? min(parts, kMostParts) : 1;
 }
 
-size_t sample_ws_bytes(int T, int V)
+// 32-bit logits
+static int sample_float_parts(int T, int V) { return T <= 96 ? min(8, V / 8192) : 1; }
+
+size_t sample_ws_bytes(int T, int V)        // (of either type)
 {
     const int parts = sample_parts(T, V);
-    return parts > 1 ? (size_t)T * parts * sizeof(PartCounts) : 0;
+    const size_t values = parts > 1 ? (size_t)T * parts * sizeof(PartCounts) : 0, floats = sample_float_parts(T, V) > 1 ? (size_t)T * sizeof(FloatRow) : 0;
+    return values > floats ? values : floats;
 }
 
 template <int NQ>
@@ -1294,9 +1480,22 @@ static int launch_choose(const SampleArgs &a, int parts, hipStream_t s)
 int launch_sample(const SampleArgs &a, hipStream_t s)
 {
     if (a.f32) {
-        static LdsLimitOnce once;
-        int rc = raise_lds_limit((const void *)sample_floats_kernel, once, "sample_floats_kernel");
-        if (rc) return rc;
+        static LdsLimitOnce once[3];
+        const int parts = sample_float_parts(a.T, a.V);
+        int rc;
+        if (parts > 1) {
+            if ((rc = raise_lds_limit((const void *)sample_float_bins_kernel, once[0], "sample_float_bins_kernel")) ||
+                (rc = raise_lds_limit((const void *)sample_float_choose_kernel, once[1], "sample_float_choose_kernel")))
+                return rc;
+            const dim3 grid((unsigned)(a.T * parts)), block(kRowThreads);
+            sample_float_tops_kernel<<<grid, block, 0, s>>>(a, parts);
+            if ((rc = check_hip(hipGetLastError(), "sample_float_tops_kernel"))) return rc;
+            sample_float_bins_kernel<<<grid, block, sizeof(FloatLds), s>>>(a, parts);
+            if ((rc = check_hip(hipGetLastError(), "sample_float_bins_kernel"))) return rc;
+            sample_float_choose_kernel<<<dim3((unsigned)a.T), block, sizeof(WideLds), s>>>(a, parts);
+            return check_hip(hipGetLastError(), "sample_float_choose_kernel");
+        }
+        if ((rc = raise_lds_limit((const void *)sample_floats_kernel, once[2], "sample_floats_kernel"))) return rc;
         sample_floats_kernel<<<dim3((unsigned)a.T), dim3(kRowThreads), sizeof(WideLds), s>>>(a);
         return check_hip(hipGetLastError(), "sample_floats_kernel");
     }
