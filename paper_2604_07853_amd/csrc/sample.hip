@@ -1437,18 +1437,19 @@ __global__ __launch_bounds__(kRowThreads) void sample_float_choose_kernel(Sample
     float_choice(a, r, ask, row, x, s, lds);
 }
 
-// Parts of a row: none where there are rows enough, or little of them.  (Rows of 151936, us, in 1 / 4 / 8 / 16 parts: 1 row 20.8 / 17.8 / 16.2 / 16.3, 32 rows 22.4 /
-// 19.7 / 17.7 / 19.0, 64 rows 22.0 / 20.5 / 19.7 / 22.0, 128 rows 23.9 / 24.0 / 25.9, 256 rows 28.2 / 33.5.)
+// Parts of a row: none where there are rows enough, or little of them.  (Whole / in 8 parts, us: 1 row of 32003 11.7 / 14.0, of 65000 14.0 / 14.3, of 151936 21.5 / 16.9, 64 rows of
+// 151936 23.4 / 20.5, 96 rows 23.6 / 23.5; 4 and 16 parts: 1 row 18.6 and 16.7, 64 rows 21.1 and 22.4.)
 static int sample_parts(int T, int V)
 {
     const int pieces = (V + 14) / 8;        // (a row may begin anywhere in its first piece)
-    int parts = T <= 96 ? min(8, pieces / 1024) : 1;
+    int parts = T <= 64 && pieces >= 10240 ? 8 : 1;
     if (pieces > 4 * 5 * kRowThreads) parts = max(parts, (pieces + 8 * 512 - 1) / (8 * 512));       // longer than a workgroup takes
-    return parts > 1 ? min(parts, kMostParts) : 1;
+    return min(parts, kMostParts);
 }
 
-// 32-bit logits
-static int sample_float_parts(int T, int V) { return T <= 96 ? min(8, V / 8192) : 1; }
+// 32-bit logits: three launches instead of one, and the sums in memory between them.  (One row of 32003 as it is / in 7 parts 25.9 / 22.5 us, 37 rows 28.4 / 35.9; rows of 151936
+// as they are / in 8: 1 row 80.7 / 35.4, 64 rows 94.0 / 73.3, 96 rows 94.0 / 89.7.)
+static int sample_float_parts(int T, int V) { return T <= 64 && V >= 65536 ? min(min(kMostParts, V / 16384), 512 / T) : 1; }
 
 size_t sample_ws_bytes(int T, int V)        // (of either type)
 {
