@@ -441,6 +441,7 @@ constexpr double kLowest = 128.0;           // 2^7: sixteen powers of two on
 constexpr int kSide = 2048;                 // bins of a sign
 constexpr int kSlots = 2 * kSide;           // of both, by size, the signs side by side
 constexpr int kRare = 1024;                 // room for values of a sign below 2^-9 other than zero (one of 2800 tokens of logits that spread by 2.2)
+constexpr int kFront = 256;                 // of 32-bit logits up to here the first tokens of the order are sorted together
 constexpr uint32_t kNone = 0xff80ff80u;     // two -inf
 constexpr int kMostParts = 32, kPartRare = 256, kRuns = 8;
 enum { kBad = 1, kHigh = 2, kLow = 4 };
@@ -582,7 +583,8 @@ struct Chooser {
     float m;
     double inv_t;
     int calls;
-    uint32_t gathered;                          // 32-bit logits: the bin whose tokens are in the third list
+    uint32_t list_before, list_count;           // 32-bit logits: the tokens of the order that are in the third list
+    unsigned long long list_mass;
     bool lost;                                  // 32-bit logits: a bin's tokens are more than there is room for
 
     // 32-bit logits are weighed one by one: y = k ln 2 / 64 + r, the power series of e^r up to r^4 within 4e-14, 2^(k / 64) out of a table.  (y below -31: no unit.)
@@ -659,24 +661,32 @@ struct Chooser {
         __syncthreads();
     }
 
-    // 32-bit logits: the tokens of a bin into the third list.  (The last that was done with the list ended with a barrier.)
-    __device__ __forceinline__ void gather(uint32_t pattern)
+    // 32-bit logits: the tokens of a bin into the third list; a few more of them with all that stand in front, for later places lie further in front.
+    // False: there is no room for those of the bin.  (The last that was done with the list ended with a barrier.)
+    __device__ __forceinline__ bool gather(const Place &bin, bool last)
     {
-        if (gathered == pattern) return;        // (they are there)
-        gathered = pattern;
+        if (bin.before >= list_before && bin.before + bin.equal <= list_before + list_count) return true;       // (they are there)
+        const bool all = !last && bin.before + bin.equal <= (uint32_t)kFront;
+        list_before = all ? 0 : bin.before;
+        list_count = all ? bin.before + bin.equal : bin.equal;
+        list_mass = all ? 0 : bin.mass;
+        if (list_count > (uint32_t)kRare) return false;
+        const uint32_t one = bin.key << 16 ^ (bin.key >> 15 ? 0u : 0x7fffffffu), other = one ^ 0xffffu, lo = all ? 0 : min(one, other), hi = max(one, other);
         if (threadIdx.x == 0) s.in_bin = s.bin_sorted = 0;
         __syncthreads();
         row.all([&](int index, float z) {
-            if (__float_as_uint(z) >> 16 == pattern) {
+            const uint32_t k = order_key(z);
+            if (k >= lo && k <= hi) {
                 const uint32_t at = atomicAdd(&s.in_bin, 1u);
-                if (at < (uint32_t)kRare) s.list[2][at] = (unsigned long long)order_key(z) << 32 | (uint32_t)index;
+                if (at < (uint32_t)kRare) s.list[2][at] = (unsigned long long)k << 32 | (uint32_t)index;
             }
         });
         __syncthreads();
+        return true;
     }
 
     template <typename Fn>
-    __device__ __forceinline__ Place find(Fn pass, bool &listed)
+    __device__ __forceinline__ Place find(Fn pass, bool &listed, bool last = false)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = calls++ & 1;     // (what the call before has found may still be read)
         bool hit_here = false;
@@ -715,14 +725,12 @@ struct Chooser {
         }
         Place p = s.place[half][__ffs((int)hits) - 1];
         if (F32) {
-            gather(p.key);
-            const uint32_t n = s.in_bin;
-            if (n > (uint32_t)kRare) {
+            if (!gather(p, last)) {
                 lost = true;
                 return p;
             }
             listed = true;
-            among(s, s.list[2], n, &s.bin_sorted, p.before, p.mass, m, inv_t, pass);
+            among(s, s.list[2], list_count, &s.bin_sorted, list_before, list_mass, m, inv_t, pass);
             return s.spot;
         }
         p.key = order_key(pattern_value(p.key));
@@ -735,7 +743,7 @@ struct Chooser {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & (kRowWaves - 1);
         calls = 0;
         lost = false;
-        gathered = 0xffffffffu;
+        list_before = list_count = 0;
         const uint32_t n_rare[2] = {min(s.rare[0], (uint32_t)kRare), min(s.rare[1], (uint32_t)kRare)};
         double w = 0.0;
         uint32_t csum = 0;
@@ -867,14 +875,14 @@ struct Chooser {
         if (F32 && lost) return false;
         const double goal = (ask.u >= 0.f ? fmin((double)ask.u, 1.0) : 0.0) * (double)kept;
         const unsigned long long below = (unsigned long long)goal;
-        Place p = find([below](uint32_t, unsigned long long x) { return x > below; }, listed);
+        Place p = find([below](uint32_t, unsigned long long x) { return x > below; }, listed, true);
         if (F32 && lost) return false;
         if (p.there && p.before < n) {
             out.nth = p.each ? (uint32_t)fmin(fmax(floor((goal - (double)p.mass) / (double)p.each), 0.0), (double)(p.equal - 1)) : 0u;
             out.nth = min(out.nth, n - 1 - p.before);
         } else {        // the last one of any weight
             const unsigned long long all = kept;
-            p = find([all](uint32_t, unsigned long long x) { return x >= all; }, listed);
+            p = find([all](uint32_t, unsigned long long x) { return x >= all; }, listed, true);
             if (F32 && lost) return false;
             out.nth = (uint32_t)((kept - p.mass - 1) / p.each);
         }

@@ -77,6 +77,20 @@ def test_large_vocabularies_and_mixed_rows(q, dtype):
         check(z, ask(q, z, u, **ways), u, **ways)
 
 
+@pytest.mark.parametrize("offset", [0.0, -0.02, -9.0, 20.0])
+@pytest.mark.parametrize("top_k", [2, 100, 255, 256, 257, 400, 1500])
+def test_places_found_one_in_front_of_the_other(q, top_k, offset):
+    """Logits in 32 bits: the first k tokens, those of them that hold p, the token: each place lies in front of the one before, among the same tokens or not."""
+    T, V = 12, 32003
+    z = rows_of(T, V, "wide", torch.float32, top_k)
+    z[T // 2:] *= 0.01                                  # a few bins hold all
+    z = z + offset
+    z[1::2] = (z[1::2] * 4096).round() / 4096           # some equal ones
+    u = torch.linspace(0.0, 1.0, T)
+    for ways in (dict(top_k=top_k), dict(top_k=top_k, top_p=0.5), dict(top_k=top_k, top_p=0.97, min_p=0.02), dict(top_p=0.01, min_p=0.9)):
+        check(z, ask(q, z, u, **ways), u, **ways)
+
+
 @pytest.mark.parametrize("T", [1, 2, 63, 300, 1500])
 def test_many_rows(q, T):
     z = rows_of(T, 501, "wide", torch.bfloat16, T)
