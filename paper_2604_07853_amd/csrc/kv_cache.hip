@@ -89,7 +89,9 @@ int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, co
 // leave the page's first cache row in LDS; then all threads copy.
 // 8 x 18432 positions of e4m3, 458 MB: 93.8 us with 32 rows and cached accesses, 86.3 with 16 and accesses that bypass the caches (5.3 TB/s); 37 short
 // sequences, 39 MB: 9.5 us cached, 10.4 past the caches: those are for calls that would not stay in them.  Calls of few rows take four a workgroup: more of them
-// wait for lengths and pages at once.
+// wait for lengths and pages at once (37 sequences of 15 positions in e4m3 4.7 -> 3.7 us, of 150 in bf16 5.6 -> 5.5, of 260 7.3 -> 8.5).  Many sequences' search begins
+// among some of the offsets in LDS (300 of 30 in bf16 8.0 -> 7.1; 37 of 15 4.0 -> 4.2).
+constexpr int kReadFew = 6144, kReadDirect = 64;
 constexpr int64_t kReadCached = (int64_t)64 << 20;
 
 template <int D, int FMT, bool NT, int kReadRows>
@@ -99,23 +101,29 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvArgs c, const int
 {
     constexpr int kChunks = D / 8;
     __shared__ int64_t from[kReadRows];     // cache row of head 0, or -1
-    __shared__ int32_t every[kKvThreads + 1];           // the offset of every `step`-th sequence, and the end: the search begins in LDS
+    __shared__ int32_t every[kKvThreads + 1];           // the offset of every `step`-th sequence, and the end
     const int64_t row0 = (int64_t)blockIdx.x * kReadRows;
     const int step = (S + kKvThreads - 1) / kKvThreads;
-    for (int i = threadIdx.x; i <= kKvThreads; i += kKvThreads) every[i] = S > 0 ? offsets[min((int64_t)i * step, (int64_t)S)] : 0;
-    __syncthreads();
+    const bool many = S > kReadDirect;
+    if (many) {
+        for (int i = threadIdx.x; i <= kKvThreads; i += kKvThreads) every[i] = offsets[min((int64_t)i * step, (int64_t)S)];
+        __syncthreads();
+    }
     if (threadIdx.x < kReadRows) {
         const int64_t row = row0 + threadIdx.x;
         int64_t at = -1;
-        if (row < total && S > 0 && row >= every[0] && row < every[kKvThreads]) {
-            int lo = 0, hi = kKvThreads;    // every[lo] <= row < every[hi]
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (every[mid] <= row) lo = mid;
-                else hi = mid;
+        if (row < total && S > 0 && row >= offsets[0] && row < offsets[S]) {
+            int lo = 0, hi = S;
+            if (many) {
+                hi = kKvThreads;            // every[lo] <= row < every[hi]
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (every[mid] <= row) lo = mid;
+                    else hi = mid;
+                }
+                hi = min(hi * step, S);     // offsets[lo] <= row < offsets[hi]
+                lo *= step;
             }
-            hi = min(hi * step, S);         // offsets[lo] <= row < offsets[hi]
-            lo *= step;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (offsets[mid] <= row) lo = mid;
@@ -167,7 +175,7 @@ int launch_kv_read(const KvArgs &c, const int32_t *table, int64_t table_stride, 
                    int64_t total, void *k_out, void *v_out, hipStream_t s)
 {
     const bool nt = total * c.kv_heads * c.head_dim * (c.fmt == QARL_KV_BF16 ? 8 : c.fmt == QARL_KV_E4M3 ? 6 : 5) > kReadCached;
-    const int rows = total <= 16384 && !nt ? 4 : 16;
+    const int rows = total <= kReadFew && !nt ? 4 : 16;
     const int64_t blocks = (total + rows - 1) / rows;
     if (blocks > 0x7fffffffLL) {
         set_error("qarl_kv_cache_read: %lld rows exceed the grid limit", (long long)total);

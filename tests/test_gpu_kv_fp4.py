@@ -107,6 +107,37 @@ def test_read(q, heads, dim, page, lens):
         assert torch.equal(got.double().cpu(), want)
 
 
+@pytest.mark.parametrize("fmt", ["QARL_KV_BF16", "QARL_KV_E4M3", "QARL_KV_E2M1"])
+@pytest.mark.parametrize("S,longest", [(64, 30), (65, 30), (256, 2), (257, 70), (600, 3), (1500, 40)])
+def test_read_of_many_sequences(q, fmt, S, longest):
+    """Each row is the one that a read of the pages in their own order has there; some sequences are empty, two rows stand behind the last."""
+    page, heads, dim = 16, 2, 64
+    g = torch.Generator().manual_seed(S)
+    lens = torch.randint(0, longest + 1, (S,), generator=g)
+    lens[::7] = 0
+    width = -(-longest // page)
+    table = torch.randperm(S * width, generator=g).to(torch.int32).view(S, width)
+    c = q.KVCache.empty(getattr(q, fmt), S * width, page, heads, dim)
+    if fmt == "QARL_KV_BF16":
+        for t in (c.k, c.v):
+            t.copy_(torch.randn(t.shape, generator=g))
+    else:
+        for t in (c.k, c.v):
+            t.copy_(torch.randint(0, 120, t.shape, generator=g))
+        for t in (c.k_scales, c.v_scales):
+            t.copy_(torch.randint(100, 140, t.shape, generator=g))
+    n = S * width * page
+    whole = q.qarl_kv_cache_read(c, torch.arange(S * width, dtype=torch.int32, device="cuda")[None], torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), lens.cumsum(0)])
+    total = int(offsets[-1]) + 2
+    got = q.qarl_kv_cache_read(c, table.cuda(), offsets.to(torch.int32).cuda(), total)
+    seq = torch.repeat_interleave(torch.arange(S), lens)
+    at = torch.arange(total - 2) - offsets[seq]
+    rows = (table[seq, at // page].to(torch.int64) * page + at % page).cuda()
+    for have, all_rows in zip(got, whole):
+        assert torch.equal(have[:-2], all_rows[rows]) and not have[-2:].any()
+
+
 # ---- attention ----
 
 @pytest.mark.parametrize("heads,kv_heads,dim,page", SHAPES)
