@@ -438,13 +438,14 @@ int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_h
  *   top_k[t] > 0       its first top_k tokens
  *   top_p[t] < 1       of those the shortest beginning that holds at least top_p of their weight
  *   min_p[t] > 0       tokens with w_i >= min_p (relative to the most likely one)
- * token[t] is the first kept token at which the running sum of the weights exceeds u * (weight of the kept) (the last kept one for u >= 1, the first for u < 0
- * or NaN).  temperature[t] == 0: the first token, log-probs those of temperature 1.
+ * token[t] is the first kept token at which the running sum of the weights exceeds u * (weight of the kept) (u >= 1: the last kept one that weighs a unit,
+ * see below; u < 0 or NaN: the first).  temperature[t] == 0: the first token, log-probs those of temperature 1.
  *   logprob[t]       ln of the token's share of all V: the sampler's log-prob that qarl_logprob_mismatch compares (may be NULL)
  *   kept_logprob[t]  ln of its share of what is kept (may be NULL)
  * temperature, top_k, top_p and min_p may each be NULL (1, and no truncation).  A row with a NaN or +inf, without a finite logit, or with a temperature
  * that is negative, infinite or NaN gets token -1 and NaN.  A logit of -inf is never chosen.
  * Weights are computed in 64 bits and summed in 64-bit integers in units of 2^-43 of the largest: a row's result does not depend on timing or on the other rows.
+ * A token of less than half a unit weighs nothing: it counts for top_k and is never chosen.
  * ws: qarl_sample_workspace_bytes(T, V) bytes, 16-byte aligned; what it holds before the call does not matter.
  * Supported: V <= 2^20.  T == 0 is a no-op. */
 size_t qarl_sample_workspace_bytes(int T, int V);

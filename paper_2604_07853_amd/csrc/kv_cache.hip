@@ -2,6 +2,8 @@
 // Layout [page][head][offset][head_dim]: the tokens of a page and head lie behind one another, which is what attention streams.
 // Both kernels are bound by memory; a thread moves eight elements of k and the same eight of v.  Writing 16384 tokens of 4 x 128 in bf16 (67 MB, which the
 // last-level cache holds) takes 11.4 us, 5.9 TB/s; 256 tokens in e4m3 4.1 us, which is the launch.
+// e2m1: a scale for each quarter of a row, 2^e with the smallest e for which the quarter's largest size is at most 6 2^e: the matrix and conversion instructions
+// take such a byte as it is, and codes times scale are exact in bf16.
 #include "common.hpp"
 
 namespace qarl {

@@ -1,6 +1,8 @@
 // Rotary positions of queries and keys, and their append to the paged cache with the rotation on the way.
 // Bound by memory: an element is read and written once.  A workgroup takes a few tokens: its threads make the tokens' cosines and sines once, in LDS; then each
 // keeps those of its pairs in registers (eight of 16-bit elements, four of 32) and goes over the token's heads, two runs of 16 bytes a time.
+// 16384 tokens of 32 + 4 heads of 128 in bf16, 302 MB: 57.1 us, 5.3 TB/s (cached accesses 64); 1733 of 28 + 4 in fp32, 57 MB, which the last-level cache holds: 9.8 us.
+// With the append: 16384 tokens to a bf16 cache, 336 MB: 64.6 us, 5.2 TB/s; 256 to an e4m3 one 6.1 us, of which 4 are any launch's.
 #include "rope.hpp"
 
 namespace qarl {

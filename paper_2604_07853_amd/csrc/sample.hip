@@ -11,6 +11,11 @@
 // 16-bit logits have few values: 4096 bins hold those of size 2^-9 to 2^7 one by one, so that a count says all of a bin, weights are computed once a value
 // and not once a token, and a place in the order is a bin and a number.  32-bit logits are put into the same bins by their upper halves: these get weights beside
 // their counts, and the tokens of a bin that a place lies in are gathered and sorted.  Rows whose other values matter take a general way, which asks for nothing.
+//
+// A row is read from memory once, and once more in part to find its token.  What bounds it: 16-bit rows of 151936, 256 of them (78 MB): 27.3 us, of which counting
+// 17.5 (4.4 TB/s, 1024 threads a CU that wait for the LDS), the choice 4 to 5 (some 200 instructions a wavefront between ten barriers), the token's search 3; with top-k
+// and top-p 28.6.  One such row, in parts: 16.6 and 18.2.  32-bit rows are bound by the 64-bit arithmetic of a weight a token: 37 of 32003 27.1 and 31.6 us, 256 of
+// 151936 114 and 111.  The general way: 256 rows of 151936 222 us in 16 bits, 240 to 314 in 32.  (In a captured graph.)
 #include <stddef.h>
 
 #include <type_traits>
@@ -441,7 +446,8 @@ constexpr double kLowest = 128.0;           // 2^7: sixteen powers of two on
 constexpr int kSide = 2048;                 // bins of a sign
 constexpr int kSlots = 2 * kSide;           // of both, by size, the signs side by side
 constexpr int kRare = 1024;                 // room for values of a sign below 2^-9 other than zero (one of 2800 tokens of logits that spread by 2.2)
-constexpr int kFront = 256;                 // of 32-bit logits up to here the first tokens of the order are sorted together
+constexpr int kRankLanes = 8, kRanked = kRowThreads / kRankLanes;   // lists up to here are sorted by counting (37 rows of 32003 29.3 -> 27.1 us)
+constexpr int kFront = kRanked;             // of 32-bit logits up to here the first tokens of the order are sorted together (with top-k and top-p 36.5 -> 33.3 us)
 constexpr uint32_t kNone = 0xff80ff80u;     // two -inf
 constexpr int kMostParts = 32, kPartRare = 256, kRuns = 8;
 enum { kBad = 1, kHigh = 2, kLow = 4 };
@@ -455,7 +461,7 @@ struct PartCounts {
 
 struct ChooseLds {
     uint32_t bins[2][kSlots];               // a row's quarters, two to a word (row by row); the first half: a part's counts
-    unsigned long long list[3][kRare];      // the rare values by sign: key and index; 32-bit logits: those of one bin
+    unsigned long long list[3][kRare];      // the rare values by sign: key and index; 32-bit logits: those of one bin, or the order's first ones
     unsigned long long wave_mass[kRowWaves], rare_mass[2], rare_sum[kRowWaves];
     uint32_t wave_count[kRowWaves], wave_first[kRowWaves], wave_hit[2][kRowWaves];
     uint32_t rare[2], sorted[2], flags, n_min, top, zeros[kMostParts], in_bin, bin_sorted;
@@ -618,7 +624,20 @@ struct Chooser {
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         __syncthreads();
-        if (!*sorted) {
+        if (!*sorted && n <= (uint32_t)kRanked) {       // eight lanes count what stands in front of a token
+            const uint32_t token = threadIdx.x / kRankLanes;
+            const unsigned long long x = token < n ? list[token] : 0;
+            uint32_t rank = 0;
+            if ((uint32_t)(wave * 64 / kRankLanes) < n) {
+                for (uint32_t j = threadIdx.x % kRankLanes; j < n; j += kRankLanes) rank += list[j] < x;
+#pragma unroll
+                for (int o = kRankLanes / 2; o > 0; o >>= 1) rank += (uint32_t)__shfl_xor((int)rank, o, 64);
+            }
+            __syncthreads();
+            if (token < n && threadIdx.x % kRankLanes == 0) list[rank] = x;
+            __syncthreads();
+            if (threadIdx.x == 0) *sorted = 1;
+        } else if (!*sorted) {
             uint32_t size = 2;
             while (size < n) size *= 2;
             if (threadIdx.x >= n && threadIdx.x < size) list[threadIdx.x] = ~0ull;
