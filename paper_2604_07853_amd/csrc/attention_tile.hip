@@ -13,9 +13,9 @@
 //
 // Measured, 32 query heads on 4 cached ones of 128, calls on end: eight prompts of 2048 bf16 352 us (275 GFLOP, 781 TFLOP/s), e4m3 384 (716), with a window of
 // 512 210 (572), head_dim 64 236 (584); 4 x 2048 over 16384 cached positions 2288 us (1021 TFLOP/s); 28 heads on 4, 12 chunks of mixed lengths over an e4m3
-// cache 332 us (781 TFLOP/s), 12 chunks of 1 to 700 queries over up to
-// 8192 positions of an e2m1 one 295 (879 TFLOP/s: nothing is rescaled).  The first ten calls after a pause of 50 ms take 438 us for the prompts and 419 for the chunks; under the profiler 384 and 345.  A
-// tile takes 4040-4160 cycles, 2048 of them products; a block 7 us more to start and end.
+// cache 332 us (781 TFLOP/s), 12 chunks of 1 to 700 queries over up to 8192 positions of an e2m1 one 295 (879 TFLOP/s: nothing is rescaled).  The first ten
+// calls after a pause of 50 ms take 438 us for the prompts and 419 for the chunks; under the profiler 384 and 345.  A tile takes 4040-4160 cycles, 2048 of them
+// products; a block 7 us more to start and end.
 #include "attention.hpp"
 
 namespace qarl {

@@ -15,7 +15,8 @@
 // A row is read from memory once, and once more in part to find its token.  What bounds it: 16-bit rows of 151936, 256 of them (78 MB): 27.3 us, of which counting
 // 17.5 (4.4 TB/s, 1024 threads a CU that wait for the LDS), the choice 4 to 5 (some 200 instructions a wavefront between ten barriers), the token's search 3; with top-k
 // and top-p 28.6.  One such row, in parts: 16.6 and 18.2.  32-bit rows are bound by the 64-bit arithmetic of a weight a token: 37 of 32003 27.1 and 31.6 us, 256 of
-// 151936 114 and 111.  The general way: 256 rows of 151936 222 us in 16 bits, 240 to 314 in 32.  (In a captured graph.)
+// 151936 114 and 111; a place among more than 1024 tokens of one upper half costs another passage (3 rows of 2^20 141 us, by the general way 908).  The general
+// way: 256 rows of 151936 222 us in 16 bits, 240 to 314 in 32.  (In a captured graph.)
 #include <stddef.h>
 
 #include <type_traits>
@@ -591,7 +592,7 @@ struct Chooser {
     int calls;
     uint32_t list_before, list_count;           // 32-bit logits: the tokens of the order that are in the third list
     unsigned long long list_mass;
-    bool lost;                                  // 32-bit logits: a bin's tokens are more than there is room for
+    bool lost;                                  // 32-bit logits: sixteen keys' tokens are more than there is room for
 
     // 32-bit logits are weighed one by one: y = k ln 2 / 64 + r, the power series of e^r up to r^4 within 4e-14, 2^(k / 64) out of a table.  (y below -31: no unit.)
     __device__ static __forceinline__ unsigned long long weigh_by(const Lds &s, double y, double &w)
@@ -680,17 +681,65 @@ struct Chooser {
         __syncthreads();
     }
 
-    // 32-bit logits: the tokens of a bin into the third list; a few more of them with all that stand in front, for later places lie further in front.
-    // False: there is no room for those of the bin.  (The last that was done with the list ended with a barrier.)
-    __device__ __forceinline__ bool gather(const Place &bin, bool last)
+    // 32-bit logits, a bin of more tokens than there is room for: counted again by the next twelve bits of their keys.  The sixteen keys in which the place
+    // lies in s.spot, the first of them as its key, their weight in place of one's.
+    template <typename Fn>
+    __device__ static __attribute__((noinline)) void narrow(Lds &s, Row<F32> row, uint32_t lo, uint32_t before, unsigned long long mass, float m, double inv_t, Fn pass)
     {
-        if (bin.before >= list_before && bin.before + bin.equal <= list_before + list_count) return true;       // (they are there)
+        if constexpr (F32) {
+            const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = (int)threadIdx.x * kEach;
+            static_assert(kEach == 4 && 16 * kEach * kRowThreads == 1 << 16, "a bin's keys");
+            *(u32x4 *)(s.bins[0] + first) = ((u32x4 *)(s.mass + first))[0] = ((u32x4 *)(s.mass + first))[1] = u32x4{0, 0, 0, 0};
+            __syncthreads();
+            row.all([&](int, float z) {
+                const uint32_t k = order_key(z) - lo;
+                if (k >> 16 == 0) {
+                    double w;
+                    const unsigned long long units = weigh_by(s, ((double)z - (double)m) * inv_t, w);
+                    atomicAdd(&s.bins[0][k >> 4], 1u);
+                    if (units) atomicAdd(&s.mass[k >> 4], units);
+                }
+            });
+            __syncthreads();
+            uint32_t csum = 0;
+            unsigned long long wsum = 0;
+            for (int i = 0; i < kEach; ++i) {
+                csum += s.bins[0][first + i];
+                wsum += s.mass[first + i];
+            }
+            const uint32_t ci = scan_lanes<true>(csum);
+            const unsigned long long wi = scan_lanes<true>(wsum);
+            if (lane == 63) {
+                s.wave_count[wave] = ci;
+                s.wave_mass[wave] = wi;
+            }
+            __syncthreads();
+            const uint32_t wc = s.wave_count[lane & (kRowWaves - 1)], wcs = scan_lanes<false>(wc);
+            const unsigned long long wm = s.wave_mass[lane & (kRowWaves - 1)], wms = scan_lanes<false>(wm);
+            const int at = __builtin_amdgcn_readfirstlane(wave);
+            before += ci - csum + lane_of(wcs, at) - lane_of(wc, at);
+            mass += wi - wsum + lane_of(wms, at) - lane_of(wm, at);
+            for (int i = 0; i < kEach; ++i) {
+                const uint32_t n = s.bins[0][first + i];
+                const unsigned long long w = s.mass[first + i];
+                if (n && pass(before + n, mass + w) && !pass(before, mass)) s.spot = Place{lo + 16 * (uint32_t)(first + i), before, n, mass, w, true};
+                before += n;
+                mass += w;
+            }
+            __syncthreads();
+        }
+    }
+
+    // 32-bit logits: the tokens of keys lo .. hi (a bin, or sixteen of its keys) into the third list; a few of them with all that stand in front, for later places
+    // lie further in front.  (The last that was done with the list ended with a barrier.)
+    __device__ __forceinline__ void gather(const Place &bin, uint32_t lo, uint32_t hi, bool last)
+    {
+        if (bin.before >= list_before && bin.before + bin.equal <= list_before + list_count) return;        // (they are there)
         const bool all = !last && bin.before + bin.equal <= (uint32_t)kFront;
         list_before = all ? 0 : bin.before;
         list_count = all ? bin.before + bin.equal : bin.equal;
         list_mass = all ? 0 : bin.mass;
-        if (list_count > (uint32_t)kRare) return false;
-        const uint32_t one = bin.key << 16 ^ (bin.key >> 15 ? 0u : 0x7fffffffu), other = one ^ 0xffffu, lo = all ? 0 : min(one, other), hi = max(one, other);
+        if (all) lo = 0;
         if (threadIdx.x == 0) s.in_bin = s.bin_sorted = 0;
         __syncthreads();
         row.all([&](int index, float z) {
@@ -701,7 +750,6 @@ struct Chooser {
             }
         });
         __syncthreads();
-        return true;
     }
 
     template <typename Fn>
@@ -744,10 +792,19 @@ struct Chooser {
         }
         Place p = s.place[half][__ffs((int)hits) - 1];
         if (F32) {
-            if (!gather(p, last)) {
-                lost = true;
-                return p;
+            const uint32_t one = p.key << 16 ^ (p.key >> 15 ? 0u : 0x7fffffffu), other = one ^ 0xffffu;
+            uint32_t lo = min(one, other), hi = max(one, other);
+            if (p.equal > (uint32_t)kRare) {
+                narrow(s, row, lo, p.before, p.mass, m, inv_t, pass);
+                p = s.spot;
+                lo = p.key;
+                hi = lo + 15;
+                if (p.equal > (uint32_t)kRare) {
+                    lost = true;
+                    return p;
+                }
             }
+            gather(p, lo, hi, last);
             listed = true;
             among(s, s.list[2], list_count, &s.bin_sorted, list_before, list_mass, m, inv_t, pass);
             return s.spot;

@@ -91,6 +91,18 @@ def test_places_found_one_in_front_of_the_other(q, top_k, offset):
         check(z, ask(q, z, u, **ways), u, **ways)
 
 
+@pytest.mark.parametrize("V", [20011, 200003])
+@pytest.mark.parametrize("offset,spread", [(20.0, 1.0), (-60.0, 0.05), (100.0, 1e-3)])
+def test_many_tokens_of_nearly_one_value(q, V, offset, spread):
+    """Logits in 32 bits whose upper halves hardly differ: thousands share one, with different weights; from the last of few values on, the same ones."""
+    T = 10
+    z = rows_of(T, V, "wide", torch.float32, V) * spread + offset
+    z[::3] = (z[::3] * 64).round() / 64
+    u = torch.linspace(0.0, 1.0, T)
+    for ways in (dict(), dict(top_p=0.7), dict(top_k=9000, top_p=0.6), dict(top_k=V - 1, min_p=0.3, temperature=0.05)):
+        check(z, ask(q, z, u, **ways), u, **ways)
+
+
 @pytest.mark.parametrize("T", [1, 2, 63, 300, 1500])
 def test_many_rows(q, T):
     z = rows_of(T, 501, "wide", torch.bfloat16, T)
