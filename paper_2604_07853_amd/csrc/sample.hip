@@ -375,7 +375,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, int r, RowLds &s
     if (ask.k > 0 && (uint32_t)ask.k < n) first_tokens((uint32_t)ask.k);
     if (ask.top_p < 1.f && n > 1) {
         const double goal = (double)fmaxf(ask.top_p, 0.f) * (double)kept;
-        const unsigned long long least = (unsigned long long)ceil(goal);
+        const unsigned long long least = max((unsigned long long)ceil(goal), 1ull);    // (one token at least: nothing passes in front of the first)
         const Place p = x.find([least](uint32_t, unsigned long long w) { return w >= least; });
         if (p.there) {
             const double more = p.each ? ceil((goal - (double)p.mass) / (double)p.each) : 1.0;
@@ -934,7 +934,7 @@ struct Chooser {
         if (F32 && lost) return false;
         if (ask.top_p < 1.f && n > 1) {
             const double goal = (double)fmaxf(ask.top_p, 0.f) * (double)kept;
-            const unsigned long long least = (unsigned long long)ceil(goal);
+            const unsigned long long least = max((unsigned long long)ceil(goal), 1ull);    // (one token at least: nothing passes in front of the first)
             const Place p = find([least](uint32_t, unsigned long long x) { return x >= least; }, listed);
             if (F32 && lost) return false;
             if (p.there) {

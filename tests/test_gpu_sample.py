@@ -247,3 +247,20 @@ def test_nothing_is_written_behind_the_workspace(q):
         got = q.qarl_sample(z.cuda(), u.cuda(), want_kept=True, ws=ws)
         assert (ws[need:] == 0x5a).all()
         check(z, got, u)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [2000, 32003, 200003])
+def test_a_share_of_nothing_keeps_the_first_token(q, dtype, V):
+    """top_p of zero and less, whatever the other truncations leave: also where more tokens than a list holds share the upper half of the largest logit."""
+    T = 8
+    z = rows_of(T, V, "wide", dtype, V)
+    z[1], z[2], z[3] = 5.0, -0.75, 0.0                          # all equal
+    z[4] = (rows_of(1, V, "wide", torch.float32, 1)[0] * 1e-3 + 100.0).to(dtype)
+    z[5] = (rows_of(1, V, "wide", torch.float32, 2)[0] * 1e-3 + 300.0).to(dtype)
+    z[6] = (rows_of(1, V, "wide", torch.float32, 3)[0] * 1e-3 - 2.0).to(dtype)
+    z[7, : V // 2] = -math.inf
+    u = torch.linspace(0.0, 1.0, T)
+    for share in (0.0, -0.5, -math.inf):
+        for ways in (dict(), dict(top_k=1500), dict(top_k=V - 1, temperature=0.7), dict(min_p=0.2), dict(top_k=1100, min_p=0.9, temperature=3.0)):
+            check(z, ask(q, z, u, top_p=share, **ways), u, top_p=share, **ways)
