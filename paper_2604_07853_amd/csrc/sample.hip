@@ -450,14 +450,14 @@ constexpr int kRare = 1024;                 // room for values of a sign below 2
 constexpr int kRankLanes = 8, kRanked = kRowThreads / kRankLanes;   // lists up to here are sorted by counting (37 rows of 32003 29.3 -> 27.1 us)
 constexpr int kFront = kRanked;             // of 32-bit logits up to here the first tokens of the order are sorted together (with top-k and top-p 36.5 -> 33.3 us)
 constexpr uint32_t kNone = 0xff80ff80u;     // two -inf
-constexpr int kMostParts = 32, kPartRare = 256, kRuns = 8;
+constexpr int kMostParts = 32, kRuns = 8;
 enum { kBad = 1, kHigh = 2, kLow = 4 };
 
 // What the workgroup that counts a part of a row leaves of it
 struct PartCounts {
     uint16_t count[2 * kSide];  // by size, the signs side by side: a part has at most 65535 tokens
     uint32_t zeros, flags, rare[2];
-    unsigned long long list[2][kPartRare];  // key and index of the rare values, by sign
+    unsigned long long list[2][kRare];      // key and index of the rare values, by sign: room for a whole row's, so that its way does not go by how it is cut
 };
 
 struct ChooseLds {
@@ -1132,7 +1132,7 @@ constexpr int kCountThreads = 512;
 __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(SampleArgs a, int parts)
 {
     __shared__ __align__(16) uint32_t bins[kSlots];
-    __shared__ unsigned long long list[2][kPartRare];
+    __shared__ unsigned long long list[2][kRare];
     __shared__ uint32_t rare[2], zeros, flags;
     const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = (int)threadIdx.x;
     const Row<false> row(a.logits, a.stride, r, a.V);
@@ -1150,7 +1150,7 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(SampleArgs 
     for (int i = tid; i < kSide / 2; i += kCountThreads) ((u32x4 *)bins)[i] = u32x4{0, 0, 0, 0};
     if (tid == 0) rare[0] = rare[1] = zeros = flags = 0;
     __syncthreads();
-    Counts counts{bins, rare, list[0], kPartRare, 0, 0};
+    Counts counts{bins, rare, list[0], kRare, 0, 0};
     for (int i0 = from; i0 < to; i0 += kAhead * kCountThreads) {
         if (i0 > from) load(i0);
 #pragma unroll
@@ -1165,9 +1165,8 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(SampleArgs 
         ((u32x4 *)out.count)[i] = u32x4{x[0] | x[1] << 16, x[2] | x[3] << 16, y[0] | y[1] << 16, y[2] | y[3] << 16};
     }
     if (tid == 0) *(u32x4 *)&out.zeros = u32x4{zeros, flags, rare[0], rare[1]};
-    static_assert(kCountThreads == 2 * kPartRare, "a thread for each entry");
-    const int sign = tid / kPartRare, at = tid % kPartRare;
-    if ((uint32_t)at < rare[sign]) out.list[sign][at] = list[sign][at];
+    for (int sign = 0; sign < 2; ++sign)
+        for (uint32_t i = tid; i < min(rare[sign], (uint32_t)kRare); i += kCountThreads) out.list[sign][i] = list[sign][i];
 }
 
 // ... and put together by one, which chooses and looks for the token in the part that holds it
@@ -1227,9 +1226,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_choose_kernel(SampleArgs a
             const uint32_t n = head[j][2 + sign];
             if (n == 0) continue;
             uint32_t base = 0;
-            if (lane == 0) base = atomicAdd(&s.rare[sign], n <= (uint32_t)kPartRare ? n : (uint32_t)kRare + 1);
+            if (lane == 0) base = atomicAdd(&s.rare[sign], n <= (uint32_t)kRare ? n : (uint32_t)kRare + 1);
             base = lane_of(base, 0);
-            if (n > (uint32_t)kPartRare) continue;
+            if (n > (uint32_t)kRare) continue;
             for (uint32_t i = lane; i < n; i += 64)
                 if (base + i < (uint32_t)kRare) s.list[sign][base + i] = i < 64 ? early[j][sign] : of[p].list[sign][i];
         }

@@ -264,3 +264,27 @@ def test_a_share_of_nothing_keeps_the_first_token(q, dtype, V):
     for share in (0.0, -0.5, -math.inf):
         for ways in (dict(), dict(top_k=1500), dict(top_k=V - 1, temperature=0.7), dict(min_p=0.2), dict(top_k=1100, min_p=0.9, temperature=3.0)):
             check(z, ask(q, z, u, top_p=share, **ways), u, top_p=share, **ways)
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.bfloat16, 81920), (torch.bfloat16, 163000), (torch.float32, 65536), (torch.float32, 90001)])
+def test_a_row_does_not_depend_on_how_many_there_are(q, dtype, V):
+    """Up to 64 rows are cut into parts, more are not: the same tokens and log-probs, bit for bit.  Rows 0 to 7 of 16 bits: more values below 2^-9 in one part than
+    others hold in all; temperatures at which the weight of a value three steps below the largest lies so near a border between two units that an exponential
+    and a product of three factors fall on either side of it, and random numbers between the two sums that follow: any change of way shows in the token."""
+    T = 65
+    z = rows_of(T, V, "wide", dtype, V)
+    z[8:12] = rows_of(4, V, "flat", dtype, 1)
+    u, t = torch.rand((T,), generator=torch.Generator().manual_seed(V)), torch.ones(T)
+    if V == 163000:
+        z[:8, :300] = 2.0 ** -10
+        z[:8, 300:80300] = 5.09375
+        z[:8, 80300:] = 5.0
+        t[:8] = torch.tensor([0x3f0091f6, 0x3f00ecca, 0x3f01342c, 0x3f0091f6, 0x3f00ecca, 0x3f01342c, 0x3f0091f6, 0x3f00ecca], dtype=torch.int32).view(torch.float32)
+        u[:8] = torch.tensor([14032438, 11532833, 11334061, 14032438, 11532833, 11334061, 14032438, 11532833]) / 2.0 ** 24
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=700, min_p=0.001)):
+        way = dict(temperature=t, **kw)
+        whole = ask(q, z, u, **way)
+        for lo, hi in ((0, 64), (0, 1), (2, 9)):
+            part = ask(q, z[lo:hi], u[lo:hi], **dict(way, temperature=t[lo:hi]))
+            assert all(torch.equal(whole[n][lo:hi], part[n]) for n in whole), (kw, lo, hi, whole["token"][lo:hi].tolist(), part["token"].tolist())
+        check(z[8:], {n: v[8:] for n, v in whole.items()}, u[8:], **dict(way, temperature=t[8:]))
