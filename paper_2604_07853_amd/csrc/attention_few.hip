@@ -29,14 +29,22 @@ struct FewLayout {
     // two stages instead of four (three: 74 and 121).
     static constexpr int kRing = E2M1 ? 2 : kStage <= 5000 ? 4 : 2;
     static constexpr int kWide = E2M1 ? 4 * kFewTile * 4 : 0;            // a wavefront's scales of values as numbers
+    static constexpr int kBytes = kFewWaves * (kRing * kStage + kWide), kHeld = 4 * kBytes <= 160 * 1024 ? 4 : 160 * 1024 / kBytes;      // workgroups that a CU holds, about
     // Chunk c of row r lies at chunk c ^ swz(r): 16 rows that are read at the same chunk spread over all banks
     __device__ static constexpr int swz(int r) { return (r / (256 / kRowBytes)) & (kChunks - 1); }
 };
 
 // The sequence with the `left`-th longest cache, by sixteenths of the longest: where a CU gets several (sequence, head)s one behind the other, the long ones begin
-// first, and none of them when the others are done.  (Which workgroup takes a sequence changes no result.  256 sequences of up to 18432, four heads: e4m3 516 -> 489 us,
-// e2m1 285 -> 271; with 256 (sequence, head)s, which all begin at once, it has cost 5 %.)
-constexpr int kMostOrdered = 512;
+// first, and none of them when the others are done.  (Which workgroup takes a sequence changes no result.)
+// The search costs a workgroup 2 to 3 us, which short caches do not give back, and more than four workgroups behind one another even out by themselves.  32 query
+// heads on 4 of 128, in a captured graph, as they come / from the longest on, us:
+//   caches of 1 to 18432  256 sequences: bf16 814 / 811, e4m3 489 / 469, e2m1 286 / 267;   512: bf16 1689 / 1737, e4m3 934 / 941, e2m1 541 / 515
+//   of 1 to 8192          256: 372 / 346, 235 / 209, 154 / 122;   512: 759 / 759, 428 / 407, 268 / 229
+//   of 1 to 4096          256: 202 / 199, 129 / 117, 69 / 59;     512: 391 / 403, 220 / 215, 137 / 122
+//   of 1 to 2048          256: 109 / 115, 56 / 55, 41 / 35;       512: 199 / 232, 115 / 121, 62 / 62
+//   all of 64             256: 17.9 / 22.2, 9.9 / 12.4, 7.3 / 8.9
+// (256 (sequence, head)s, which all begin at once: 5 % slower.)  The bound of the lengths may be loose: the first 64 of them have to reach kOrderFrom too.
+constexpr int kMostOrdered = 512, kOrderFrom = 3584;
 __device__ __forceinline__ int nth_longest(const AttnArgs &a, unsigned left, int lane)
 {
     const int at = (int)left;
@@ -65,6 +73,14 @@ __device__ __forceinline__ int nth_longest(const AttnArgs &a, unsigned left, int
     return at;      // (does not happen: every sequence is in one of them)
 }
 
+// The sequence of the workgroups at place `at`
+template <int HELD>
+__device__ __forceinline__ int sequence_at(const AttnArgs &a, unsigned per_split, int at, int lane)
+{
+    if (per_split <= 512 || per_split > 4 * 256 * HELD || a.S == 1 || a.S > kMostOrdered || a.max_kv_len < kOrderFrom) return at;
+    return __ballot(a.kv_lens[min(lane, a.S - 1)] >= kOrderFrom) ? __builtin_amdgcn_readfirstlane(nth_longest(a, (unsigned)at, lane)) : at;
+}
+
 template <int D, int FMT, int NR>
 __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_kernel(AttnArgs a, int chunk, AttnParts parts)
 {
@@ -79,7 +95,7 @@ __global__ __launch_bounds__(kFewThreads, NR == 4 ? 1 : 2) void attention_few_ke
     const int split = (int)(blockIdx.x / per_split);
     const unsigned sh = blockIdx.x - (unsigned)split * per_split;
     const int s_at = (int)(sh / (unsigned)Hkv), h = (int)(sh - (unsigned)s_at * (unsigned)Hkv);
-    const int s = __builtin_amdgcn_readfirstlane(per_split > 512 && a.S > 1 && a.S <= kMostOrdered ? nth_longest(a, (unsigned)s_at, lane) : s_at);
+    const int s = sequence_at<L::kHeld>(a, per_split, s_at, lane);
     const SeqRange sr = seq_range(a, s);
     if (over_long(a, sr)) {
         if (split == 0 && parts.splits > 0) {

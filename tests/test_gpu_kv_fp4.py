@@ -342,3 +342,22 @@ def test_sequences_taken_in_the_order_of_their_lengths(q, fmt, S, kv_heads, lens
     got = call(q, m, max_kv=100000 if lens == "bound" else None, out=out)
     assert got["out"].isfinite().all()
     check(m, got)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("S,kv_heads,dim", [(130, 4, 128), (66, 8, 64), (512, 2, 64), (512, 8, 128)])
+def test_long_caches_first_or_in_their_own_order(q, fmt, S, kv_heads, dim):
+    """A few long caches among short ones: workgroups take them first where one of the first 64 sequences is long, and in the order of the call where they stand
+    behind.  Either way every sequence gets the same bits."""
+    import test_gpu_attention as base
+    n = torch.randint(0, 60, (S,), generator=torch.Generator().manual_seed(S)).tolist()
+    n[3], n[7], n[40], n[S // 2], n[S - 1] = 0, 5000, 3700, 3600, 4100
+    seqs = [(1, v) for v in n]
+    m = make(q, seqs, 2 * kv_heads, kv_heads, dim, 16, S) if fmt == "fp4" else base.make(q, fmt, seqs, 2 * kv_heads, kv_heads, dim, 16, S)
+    outs = [torch.full((S, 2 * kv_heads, dim), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    got = call(q, m, out=outs[0])
+    assert got["out"].isfinite().all()
+    check(m, got)
+    order = torch.tensor(sorted(range(S), key=lambda s: n[s]))
+    again = call(q, dict(m, query=m["query"][order], table=m["table"][order], kv_lens=m["kv_lens"][order]), out=outs[1])
+    assert torch.equal(again["out"].cpu(), got["out"].cpu()[order]) and torch.equal(again["lse"].cpu(), got["lse"].cpu()[order])
