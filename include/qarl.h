@@ -372,7 +372,7 @@ int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, i
  *     PLAIN   as they are
  *     LINEAR  f_i / factor (positions interpolated)
  *     YARN    f_i for pairs that make more than `high` turns within original_len, f_i / factor for those of less than `low`, in between linearly by the
- *             number of the pair (from the pair, rounded down, that makes `high` turns to that, rounded up, of `low`); amplitude 0.1 ln factor + 1
+ *             number of the pair (from the pair, rounded down, that makes `high` turns to that, rounded up, of `low`, rotary_dim - 1 at most); amplitude 0.1 ln factor + 1
  *     BANDS   the same ends, in between linearly by the turns themselves; amplitude 1
  *   qarl_rope_init: the descriptor, from these or from any other frequencies in [0, pi) radians a position.
  * Supported: rotary_dim % 16 == 0, rotary_dim <= 2 * QARL_ROPE_MAX_PAIRS. */

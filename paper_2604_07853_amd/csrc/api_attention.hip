@@ -210,7 +210,7 @@ int qarl_rope_frequencies(int rotary_dim, double base, int scaling, double facto
         const double f = pow(base, -2.0 * i / rotary_dim);
         double keep = 1.0;      // share of the pair's own frequency, beside the stretched one
         if (scaling == QARL_ROPE_LINEAR) keep = 0.0;
-        else if (scaling == QARL_ROPE_YARN) keep = 1.0 - fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);
+        else if (scaling == QARL_ROPE_YARN) keep = last <= 0.0 ? 0.0 : 1.0 - fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);      // (last <= 0: no pair makes `low` turns)
         else if (scaling == QARL_ROPE_BANDS) keep = fmin(fmax((original_len * f / 6.283185307179586 - low) / (high - low), 0.0), 1.0);
         inv_freq[i] = scaling == QARL_ROPE_PLAIN ? f : f * keep + f / factor * (1.0 - keep);
     }

@@ -130,3 +130,18 @@ def test_the_binding_refuses_what_is_not_on_the_gpu_or_of_another_shape(rope):
             q.KVCache(q.QARL_KV_E2M1, *bad)
     with pytest.raises(ValueError, match="even"):
         q.KVCache.empty(q.QARL_KV_E2M1, 2, 16, 4, 63, "cpu")
+
+
+@pytest.mark.parametrize("base,length,low,high", [(1e4, 4.0, 1.0, 32.0), (1e4, 1.0, 1.0, 32.0), (1e4, 6.25, 1.0, 32.0), (1e4, 40.0, 8.0, 32.0), (1e4, 200.0, 1.0, 32.0), (5.0, 300.0, 1.0, 2.0),
+                                                  (1e6, 1e17, 1.0, 32.0)])
+def test_stretched_frequencies_at_the_ends(L, base, length, low, high):
+    """Pairs of fewer than `low` turns are stretched and those of more than `high` are not, also where that is all pairs, the first among them."""
+    f, _ = q.qarl_rope_frequencies(64, base)
+    y, _ = q.qarl_rope_frequencies(64, base, q.QARL_ROPE_YARN, 8.0, length, low, high)
+    for i in range(32):
+        turns = length * f[i] / (2 * math.pi)
+        if turns > high * (1 + 1e-9):
+            assert y[i] == f[i], i
+        elif turns < low * (1 - 1e-9):
+            assert abs(y[i] - f[i] / 8) <= 1e-15 * f[i], i
+        assert f[i] / 8 * (1 - 1e-12) <= y[i] <= f[i] * (1 + 1e-12), i
