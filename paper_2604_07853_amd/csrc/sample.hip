@@ -475,9 +475,10 @@ union ValueLds {
     RowLds row;         // for rows that take the general way
 };
 struct FloatLds : ChooseLds {
-    unsigned long long mass[2 * kSide];
+    alignas(16) unsigned long long mass[2 * kSide];
     double powers[64];      // 2^(j / 64)
 };
+static_assert(alignof(FloatLds) == 16 && sizeof(PartCounts) % 16 == 0, "cleared, written and read in 16 bytes");
 union WideLds {
     FloatLds choose;
     RowLds row;
@@ -1400,6 +1401,7 @@ struct FloatRow {
     uint32_t top[kMostParts], bad[kMostParts];
     unsigned long long list[2][kRare];
 };
+static_assert(sizeof(FloatRow) % 16 == 0, "the next row's begins at 16 bytes");
 
 __global__ __launch_bounds__(kRowThreads) void sample_float_tops_kernel(SampleArgs a, int parts)
 {
