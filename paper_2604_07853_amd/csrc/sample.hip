@@ -1595,7 +1595,7 @@ int launch_sample(const SampleArgs &a, hipStream_t s)
         int rc = check_hip(hipGetLastError(), "sample_count_kernel");
         if (rc) return rc;
         const int per = (pieces + parts - 1) / parts;
-        return per <= kRowThreads ? launch_choose<1>(a, parts, s) : per <= 4 * kRowThreads ? launch_choose<4>(a, parts, s) : launch_choose<kRuns>(a, parts, s);
+        return per <= 4 * kRowThreads ? launch_choose<4>(a, parts, s) : launch_choose<kRuns>(a, parts, s);     // (1280 pieces a part or more)
     }
     const int quarter = (pieces + 3) / 4;
     if (quarter <= kRowThreads) return launch_values<1>(a, s);
