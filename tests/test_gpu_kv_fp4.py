@@ -361,3 +361,33 @@ def test_long_caches_first_or_in_their_own_order(q, fmt, S, kv_heads, dim):
     order = torch.tensor(sorted(range(S), key=lambda s: n[s]))
     again = call(q, dict(m, query=m["query"][order], table=m["table"][order], kv_lens=m["kv_lens"][order]), out=outs[1])
     assert torch.equal(again["out"].cpu(), got["out"].cpu()[order]) and torch.equal(again["lse"].cpu(), got["lse"].cpu()[order])
+
+
+@pytest.mark.parametrize("fmt", ["QARL_KV_BF16", "QARL_KV_E4M3", "QARL_KV_E2M1"])
+@pytest.mark.parametrize("dim,page", [(128, 16), (64, 128)])
+def test_large_reads_equal_small_ones(q, fmt, dim, page):
+    """Reads that move more than 64 MB pass the caches, those of up to 6144 rows take fewer rows a workgroup: the same bits, sequence by sequence and whole."""
+    heads, lens = 4, [9000, 0, 1, 14001, 5000] if dim == 128 else [20001, 0, 1, 30003, 6000]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(dim)
+    need = [-(-n // page) for n in lens]
+    c = q.KVCache.empty(getattr(q, fmt), sum(need), page, heads, dim)
+    for t in (c.k, c.v):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda") if fmt == "QARL_KV_BF16" else torch.randint(0, 127, t.shape, generator=g, device="cuda"))
+    for t in (c.k_scales, c.v_scales):
+        if t is not None:
+            t.copy_(torch.randint(100, 140, t.shape, generator=g, device="cuda"))
+    table = torch.full((len(lens), max(need)), -1, dtype=torch.int32)
+    perm = torch.randperm(sum(need), generator=torch.Generator().manual_seed(1)).to(torch.int32)
+    for s, n in enumerate(need):
+        table[s, :n] = perm[sum(need[:s]): sum(need[:s]) + n]
+    table = table.cuda()
+    offsets = torch.tensor([0] + lens, dtype=torch.int64).cumsum(0).to(torch.int32)
+    total = int(offsets[-1])
+    whole = q.qarl_kv_cache_read(c, table, offsets.cuda(), total)
+    for s, n in enumerate(lens):
+        for lo in range(0, n, 96 * page):       # (at most 12288 rows, a few pages at a time)
+            rows = min(96 * page, n - lo)
+            part = q.qarl_kv_cache_read(c, table[s: s + 1, lo // page:].contiguous(), torch.tensor([0, rows], dtype=torch.int32, device="cuda"), rows)
+            at = int(offsets[s]) + lo
+            assert all(torch.equal(a[at: at + rows], b) for a, b in zip(whole, part)), (s, lo)

@@ -302,3 +302,49 @@ def test_offsets_past_32_bits(q):
     for cache, at in ((c, slots), (small, slots - (pages - 1) * page)):
         q.qarl_rotary_kv_write(cache, rope, torch.arange(3, device="cuda"), None, x[:, :heads], x[:, heads:], at)
     assert not c.k[:4].any() and torch.equal(c.k[-1], small.k[0]) and torch.equal(c.v_scales[-1], small.v_scales[0]) and c.k[-1].any()
+
+
+def random_heads(T, heads, dim, dtype, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn((T, heads, dim), generator=g, device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout,inverse", [(0, False), (1, True)])
+def test_large_calls_equal_small_ones(q, dtype, layout, inverse):
+    """Calls that move more than 64 MB pass the caches: the bits of the same tokens in smaller calls."""
+    T, step, heads, dim = (9001, 1500, 24, 128) if dtype == torch.bfloat16 else (5001, 1000, 24, 128)
+    rope = q.Rope(96, base=1e6, layout=layout)
+    x, pos = random_heads(T, heads + 1, dim, dtype, 3), torch.arange(T, device="cuda") * 7 + 100
+    whole = q.qarl_rotary(rope, pos, x[:, :20], x[:, 20:24], inverse=inverse)
+    for lo in range(0, T, step):
+        part = q.qarl_rotary(rope, pos[lo: lo + step], x[lo: lo + step, :20], x[lo: lo + step, 20:24], inverse=inverse)
+        assert all(torch.equal(whole[n][lo: lo + step], part[n]) for n in whole), lo
+    y = x.clone()
+    q.qarl_rotary(rope, pos, y[:, :20], y[:, 20:24], inverse=inverse, q_out=y[:, :20], k_out=y[:, 20:24])
+    assert torch.equal(y[:, :20], whole["q"]) and torch.equal(y[:, 20:24], whole["k"]) and torch.equal(y[:, 24], x[:, 24])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("T,step,dim,layout", [(9001, 3000, 128, 0), (18001, 6000, 64, 1)])
+def test_large_appends_equal_small_ones(q, fmt, T, step, dim, layout):
+    heads, kv_heads, page = 16, 4, 16
+    rope = q.Rope(dim, base=1e6, layout=layout)
+    x, pos = random_heads(T, heads + 2 * kv_heads, dim, torch.bfloat16, 4), torch.arange(T, device="cuda") * 3
+    pages = T // page + 5
+    slots = torch.randperm(pages * page, generator=torch.Generator().manual_seed(T))[:T].cuda()
+    slots[::1000] = -1
+    caches, outs = [], []
+    for size in (T, step):
+        c = q.KVCache.empty(getattr(q, FMT[fmt]), pages, page, kv_heads, dim)
+        for t in (c.k, c.v, c.k_scales, c.v_scales):
+            if t is not None:
+                t.view(torch.uint8).fill_(0x5a)
+        outs.append(torch.cat([q.qarl_rotary_kv_write(c, rope, pos[lo: lo + size], x[lo: lo + size, :heads], x[lo: lo + size, heads: heads + kv_heads],
+                                                      x[lo: lo + size, heads + kv_heads:], slots[lo: lo + size]) for lo in range(0, T, size)]))
+        caches.append(c)
+    assert torch.equal(*outs)
+    for n in ("k", "v", "k_scales", "v_scales"):
+        a, b = (getattr(c, n) for c in caches)
+        assert a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8)), n

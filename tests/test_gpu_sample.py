@@ -288,3 +288,73 @@ def test_a_row_does_not_depend_on_how_many_there_are(q, dtype, V):
             part = ask(q, z[lo:hi], u[lo:hi], **dict(way, temperature=t[lo:hi]))
             assert all(torch.equal(whole[n][lo:hi], part[n]) for n in whole), (kw, lo, hi, whole["token"][lo:hi].tolist(), part["token"].tolist())
         check(z[8:], {n: v[8:] for n, v in whole.items()}, u[8:], **dict(way, temperature=t[8:]))
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.bfloat16, 32762), (torch.bfloat16, 50001), (torch.bfloat16, 65530), (torch.bfloat16, 151936), (torch.bfloat16, 163833), (torch.bfloat16, 163834),
+                                     (torch.bfloat16, 201088), (torch.float32, 65536), (torch.float32, 151936), (torch.float32, 163840)])
+def test_large_vocabularies_of_more_rows_than_are_cut(q, dtype, V):
+    """Rows of every length that one workgroup takes whole, and the first that it does not: all rows are sampled, some are checked; tokens at the row's very ends."""
+    T = 70
+    z = rows_of(T, V, "wide", dtype, V)
+    z[20:40] = rows_of(20, V, "flat", dtype, 1)
+    z[5, : V - 3], z[6, 2:] = -math.inf, -math.inf
+    z[7] = 3.0                                          # all equal: the token is the number's place
+    g = torch.Generator().manual_seed(V)
+    u = torch.rand((T,), generator=g)
+    u[7], u[8], u[9] = 0.99999, 0.0, 1.0
+    ways = dict(temperature=torch.rand((T,), generator=g) + 0.5, top_k=torch.randint(0, 3000, (T,), generator=g) * (torch.rand((T,), generator=g) < 0.5),
+                top_p=torch.rand((T,), generator=g) * 0.7 + 0.4, min_p=torch.rand((T,), generator=g) * 0.01 * (torch.rand((T,), generator=g) < 0.4))
+    ways["temperature"][1] = 0.0
+    ways["top_k"][7] = 0
+    ways["top_p"][7] = 1.0
+    pick = torch.tensor([0, 1, 5, 6, 7, 8, 9, 21, 38, 69])
+    for kw in (dict(), ways):
+        got = ask(q, z, u, **kw)
+        assert (got["token"] >= 0).all() and (got["token"] < V).all()
+        check(z[pick], {n: v[pick.cuda()] for n, v in got.items()}, u[pick], **{n: v[pick] for n, v in kw.items()})
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,V", [(1, 151936), (64, 81920), (3, 1 << 20), (70, 163834)])
+def test_workspaces_of_cut_rows(q, dtype, T, V):
+    """What a workspace holds before a call, other rows' sums among it, does not matter, and nothing is written behind it."""
+    need = q.qarl_sample_workspace_bytes(T, V)
+    assert need > 0
+    ws = torch.full((need + 65536,), 0x5a, dtype=torch.uint8, device="cuda")
+    u = torch.rand((T,), generator=torch.Generator().manual_seed(1)).cuda()
+    for i, kind in enumerate(("wide", "flat", "tiny", "wide")):
+        z = rows_of(T, V, kind, dtype, i).cuda()
+        if i == 3:
+            z[0] = math.nan
+            ws[:need] = 0xff
+        got = q.qarl_sample(z, u, want_kept=True, ws=ws)
+        clean = q.qarl_sample(z, u, want_kept=True, ws=torch.zeros((need,), dtype=torch.uint8, device="cuda"))
+        assert all(torch.equal(got[n].nan_to_num(7.0), clean[n].nan_to_num(7.0)) for n in got)
+        assert (ws[need:] == 0x5a).all()
+        lo = 1 if i == 3 and T > 1 else 0
+        check(z[lo: lo + 1].cpu(), {n: v[lo: lo + 1] for n, v in got.items()}, u[lo: lo + 1].cpu())
+
+
+@pytest.mark.parametrize("T,V", [(6, 151936), (70, 100003)])
+def test_graph_of_32_bit_logits(q, T, V):
+    z, u = rows_of(T, V, "wide", torch.float32, 1).cuda(), torch.rand((T,), device="cuda")
+    k, p = torch.randint(0, 400, (T,), dtype=torch.int32, device="cuda"), torch.full((T,), 0.9, device="cuda")
+    out = dict(token=torch.empty((T,), dtype=torch.int32, device="cuda"), logprob=torch.empty((T,), device="cuda"), kept_logprob=torch.empty((T,), device="cuda"))
+    ws = torch.full((max(16, q.qarl_sample_workspace_bytes(T, V)),), 0x5a, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        q.qarl_sample(z, u, top_k=k, top_p=p, ws=ws, **out)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q.qarl_sample(z, u, top_k=k, top_p=p, ws=ws, **out)
+    for seed in range(4):
+        z.copy_(rows_of(T, V, ("wide", "flat", "peaked", "tiny")[seed], torch.float32, 20 + seed))
+        u.copy_(torch.rand((T,)))
+        ws.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = q.qarl_sample(z, u, top_k=k, top_p=p, want_kept=True)
+        assert all(torch.equal(out[n], want[n]) for n in out)
+        check(z[:3], {n: v[:3] for n, v in out.items()}, u[:3], top_k=k[:3].cpu(), top_p=0.9)
