@@ -332,8 +332,9 @@ int qarl_add_rmsnorm_backward(const void *dy_bf16, int64_t dy_stride, const void
  *            quantizer of section 2.2 with one scale per token and head; value = scale * code.
  *   KV_E2M1: k, v uint8 [num_pages][kv_heads][page_size][head_dim / 2], two e2m1 codes a byte, the even element in the low bits (codes as for
  *            FP4_E2M1_CH), k_scales, v_scales uint8 [num_pages][kv_heads][page_size][4]: each quarter of a row (head_dim / 4 neighbouring elements) has
- *            a power of two for its scale, 2^(byte - 127), byte 255: NaN; value = scale * code.  The quantizer takes the smallest scale from 2^-100
- *            to 2^125 with 6 * scale >= absmax of the quarter and code = e2m1_rne_saturating(x / scale); a zero quarter gets 2^-100 and codes 0.
+ *            a power of two for its scale, 2^(byte - 127), byte 27 to 252, or 255: NaN; value = scale * code.  (Other bytes are never written and
+ *            stand for codes of zero alone: 253 and 254 pass the largest bf16, products with scales below 2^-100 lose bits.)  The quantizer takes the smallest scale
+ *            from 2^-100 to 2^125 with 6 * scale >= absmax of the quarter and code = e2m1_rne_saturating(x / scale); a zero quarter gets 2^-100 and codes 0.
  * Requirements: head_dim 64 or 128, page_size a power of two from 8 to 1024, kv_heads <= 1024, buffers 16-byte aligned. */
 typedef enum { QARL_KV_BF16 = 1, QARL_KV_E4M3 = 2, QARL_KV_E2M1 = 3 } qarl_kv_format;
 typedef struct {
@@ -367,7 +368,9 @@ int qarl_kv_cache_read(const qarl_kv_cache *cache, const int32_t *block_table, i
  *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
  *   ROPE_HALF:  a = x[i], b = x[rotary_dim / 2 + i];     ROPE_PAIRS:  a = x[2 i], b = x[2 i + 1]
  * Elements from rotary_dim on are passed on as they are.  The descriptor is host memory, made once and read during the call: it holds f_i / 2 pi as a 64-bit
- * fraction of a turn, so that angles are exact modulo a turn at every position (fp32 products p * f_i are not).
+ * fraction of a turn, of which p * f_i is taken modulo a turn without another rounding.  The angle is off by up to 2^-65 |p| turns (that of the fraction) and 2^-32 of
+ * a turn, its cosine and sine by some roundings to fp32 besides: up to |p| = 2^38 the first is less than a rounding to fp32, at 2^46 it is 1e-5 rad, and from 2^62 on the
+ * angle says nothing.  (fp32 products p * f_i are off by 0.008 rad at p = 131072.)
  *   qarl_rope_frequencies: f_i = base^(-2 i / rotary_dim), scaled for contexts longer than the model was trained on:
  *     PLAIN   as they are
  *     LINEAR  f_i / factor (positions interpolated)
@@ -444,7 +447,8 @@ int qarl_paged_attention(const void *q_bf16, int64_t q_token_stride, int64_t q_h
  *   kept_logprob[t]  ln of its share of what is kept (may be NULL)
  * temperature, top_k, top_p and min_p may each be NULL (1, and no truncation).  A row with a NaN or +inf, without a finite logit, or with a temperature
  * that is negative, infinite or NaN gets token -1 and NaN.  A logit of -inf is never chosen.
- * Weights are computed in 64 bits and summed in 64-bit integers in units of 2^-43 of the largest: a row's result does not depend on timing or on the other rows.
+ * Weights are computed in 64 bits, each within a unit, and summed in 64-bit integers in units of 2^-43 of the largest: a row's result does not depend on timing or on the
+ * other rows, nor on how many there are.
  * A token of less than half a unit weighs nothing: it counts for top_k and is never chosen.
  * ws: qarl_sample_workspace_bytes(T, V) bytes, 16-byte aligned; what it holds before the call does not matter.
  * Supported: V <= 2^20.  T == 0 is a no-op. */

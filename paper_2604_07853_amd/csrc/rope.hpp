@@ -1,9 +1,9 @@
 // Angles of rotary positions.
 //
 // Pair i of a head turns by p f_i at position p.  The descriptor holds f_i / 2 pi as a 64-bit fraction F_i of a turn, so that the low 64 bits of p F_i are
-// the angle modulo a whole turn: exact for every 64-bit p but for the rounding of F_i (2^-65 turns a position; fp32 products p f_i are off by 0.008 rad at
-// p = 131072).  The nearest quarter turn is taken off, the rest lies within an eighth, |x| <= pi / 4, where the power series of sine and cosine up to x^9
-// and x^10 are within 2e-9.
+// the angle modulo a whole turn, off by the rounding of F_i alone: 2^-65 turns a position, 4.7e-8 rad at p = 2^38 (fp32 products p f_i are off by 0.008 rad at
+// p = 131072).  Its upper 32 bits are kept (1.5e-9 rad).  The nearest quarter turn is taken off, the rest lies within an eighth, |x| <= pi / 4, where the power
+// series of sine and cosine up to x^9 and x^10 are within 2e-9.
 #pragma once
 #include "common.hpp"
 
