@@ -91,9 +91,10 @@ int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, co
 // leave the page's first cache row in LDS; then all threads copy.
 // 8 x 18432 positions of e4m3, 458 MB: 93.8 us with 32 rows and cached accesses, 86.3 with 16 and accesses that bypass the caches (5.3 TB/s); 37 short
 // sequences, 39 MB: 9.5 us cached, 10.4 past the caches: those are for calls that would not stay in them.  Calls of few rows take four a workgroup: more of them
-// wait for lengths and pages at once (37 sequences of 15 positions in e4m3 4.7 -> 3.7 us, of 150 in bf16 5.6 -> 5.5, of 260 7.3 -> 8.5).  Many sequences' search begins
+// wait for lengths and pages at once (37 sequences of 15 positions in e4m3 4.7 -> 3.7 us, of 150 in bf16 5.6 -> 5.5, of 260 7.3 -> 8.5; where four rows of all heads leave threads without work, as two heads of 128 do,
+// up to fewer rows: 37 of 50 in bf16 3.7 -> 3.5, 64 of 60 3.9 -> 4.0, 65 of 90 4.4 -> 4.75).  Many sequences' search begins
 // among some of the offsets in LDS (300 of 30 in bf16 8.0 -> 7.1; 37 of 15 4.0 -> 4.2).
-constexpr int kReadFew = 6144, kReadDirect = 64;
+constexpr int kReadFew = 6144, kReadFewNarrow = 2560, kReadDirect = 64;
 constexpr int64_t kReadCached = (int64_t)64 << 20;
 
 template <int D, int FMT, bool NT, int kReadRows>
@@ -177,7 +178,7 @@ int launch_kv_read(const KvArgs &c, const int32_t *table, int64_t table_stride, 
                    int64_t total, void *k_out, void *v_out, hipStream_t s)
 {
     const bool nt = total * c.kv_heads * c.head_dim * (c.fmt == QARL_KV_BF16 ? 8 : c.fmt == QARL_KV_E4M3 ? 6 : 5) > kReadCached;
-    const int rows = total <= kReadFew && !nt ? 4 : 16;
+    const int rows = total <= (4 * c.kv_heads * (c.head_dim / 8) >= kKvThreads ? kReadFew : kReadFewNarrow) && !nt ? 4 : 16;
     const int64_t blocks = (total + rows - 1) / rows;
     if (blocks > 0x7fffffffLL) {
         set_error("qarl_kv_cache_read: %lld rows exceed the grid limit", (long long)total);
