@@ -93,8 +93,8 @@ int launch_kv_write(const KvArgs &c, const void *k, int64_t kts, int64_t khs, co
 // sequences, 39 MB: 9.5 us cached, 10.4 past the caches: those are for calls that would not stay in them.  Calls of few rows take four a workgroup: more of them
 // wait for lengths and pages at once (37 sequences of 15 positions in e4m3 4.7 -> 3.7 us, of 150 in bf16 5.6 -> 5.5, of 260 7.3 -> 8.5; where four rows of all heads leave threads without work, as two heads of 128 do,
 // up to fewer rows: 37 of 50 in bf16 3.7 -> 3.5, 64 of 60 3.9 -> 4.0, 65 of 90 4.4 -> 4.75).  Many sequences' search begins
-// among some of the offsets in LDS (300 of 30 in bf16 8.0 -> 7.1; 37 of 15 4.0 -> 4.2).
-constexpr int kReadFew = 6144, kReadFewNarrow = 2560, kReadDirect = 64;
+// among some of the offsets in LDS (300 of 30 in bf16 8.0 -> 7.1, 128 of 200 of two heads 10.9 -> 10.2; 37 of 15 4.0 -> 4.2, 65 of 60 of two heads 4.0 -> 4.15).
+constexpr int kReadFew = 6144, kReadFewNarrow = 2560, kReadDirect = 96;
 constexpr int64_t kReadCached = (int64_t)64 << 20;
 
 template <int D, int FMT, bool NT, int kReadRows>

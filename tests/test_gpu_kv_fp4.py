@@ -391,3 +391,10 @@ def test_large_reads_equal_small_ones(q, fmt, dim, page):
             part = q.qarl_kv_cache_read(c, table[s: s + 1, lo // page:].contiguous(), torch.tensor([0, rows], dtype=torch.int32, device="cuda"), rows)
             at = int(offsets[s]) + lo
             assert all(torch.equal(a[at: at + rows], b) for a, b in zip(whole, part)), (s, lo)
+
+
+@pytest.mark.parametrize("fmt", ["QARL_KV_BF16", "QARL_KV_E4M3", "QARL_KV_E2M1"])
+@pytest.mark.parametrize("S,longest", [(96, 60), (97, 30), (97, 70), (200, 5), (255, 30)])
+def test_read_of_about_a_hundred_sequences(q, fmt, S, longest):
+    """Where the search for a row's sequence begins among the offsets in LDS, and fewer sequences than there is room for."""
+    test_read_of_many_sequences(q, fmt, S, longest)
