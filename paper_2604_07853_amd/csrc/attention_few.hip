@@ -2,7 +2,8 @@
 // Bound by memory: G query heads share a cached one, 4 G D operations per 4 D bytes.  A workgroup takes one (sequence, cached head, piece
 // of the cache); its four wavefronts take every fourth tile of 32 positions each, with running maxima and sums of their own, which they
 // join at the end.  (32 query heads on 4 of 128, 256 sequences of 4096 positions: bf16 361 us, 6.0 TB/s, e4m3 196 us, 5.7, e2m1 118 us, 5.1 (its loads alone
-// 109); 256 of up to 18432 e4m3 429 us, 5.6, e2m1 264, 4.7; one of 18432, where lengths, pages and keys wait for one another, 10.4 us, e2m1 9.8.)
+// 109); 256 of up to 18432, this kernel
+// alone, e4m3 429 us, 5.6, e2m1 264, 4.7; one of 18432, where lengths, pages and keys wait for one another, 10.4 us, e2m1 9.8.)
 // Keys and values flow through rings in LDS, private to a wavefront and filled by asynchronous copies, so that a wavefront waits
 // for its own copies only and no barrier stands in the loop.
 //

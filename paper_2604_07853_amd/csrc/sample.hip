@@ -14,9 +14,13 @@
 //
 // A row is read from memory once, and once more in part to find its token.  What bounds it: 16-bit rows of 151936, 256 of them (78 MB): 27.3 us, of which counting
 // 17.5 (4.4 TB/s, 1024 threads a CU that wait for the LDS), the choice 4 to 5 (some 200 instructions a wavefront between ten barriers), the token's search 3; with top-k
-// and top-p 28.6.  One such row, in parts: 16.6 and 18.2.  32-bit rows are bound by the 64-bit arithmetic of a weight a token: 37 of 32003 27.1 and 31.6 us, 256 of
-// 151936 114 and 111; a place among more than 1024 tokens of one upper half costs another passage (3 rows of 2^20 141 us, by the general way 908).  The general
-// way: 256 rows of 151936 222 us in 16 bits, 240 to 314 in 32.  (In a captured graph.)
+// and top-k 50, top-p 28.8.  One workgroup a CU: nothing is read while a row is chosen, so 512 rows take 52.4 and 1024 103 (3.0 TB/s).  Longer rows, in parts: 256 of
+// 201088 36.4 and 256000 41.2, 1024 of 256000 165.  One row of 151936, in parts: 17.4 and 19.0.  32-bit rows are read three times, for the largest, for the weights and for
+// the tokens of the bins that places lie in, and those from memory where they are many: 256 of 151936 113 and 112 us for 467 MB read (4.1 TB/s; the vector units are
+// busy 64 % of it), 1024 429 and 440; with top-p alone a fourth time, 140.  37 of 32003 27.0 and 31.9 us: few CUs, a chain of passages.  A place among more than 1024 tokens
+// of one upper half costs another passage (3 rows of 2^20 141 us, by the general way 908).  The general way reads a row for each bin and each refinement of each
+// place: 256 rows of 151936 with logits past 128 230 us in 16 bits, 250 to 320 in 32; of a thousandth's spread, whose values are all small, 530 to 730 and 640 to 880.
+// (In a captured graph.)
 #include <stddef.h>
 
 #include <type_traits>
